@@ -1,0 +1,81 @@
+// Launches of the operators on a caller's own tensors (include/pbg_operators.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+// element types (PBG_TYPE_*)
+enum { OT_F32 = 0, OT_BF16 = 1, OT_F16 = 2 };
+
+inline int type_bytes(int type) { return type == OT_F32 ? 4 : 2; }
+
+// bits of the device-side argument checks
+enum { OPS_BAD_OFFSETS = 1, OPS_BAD_LABEL = 2 };
+
+// offsets[0..groups] nondecreasing and within [0, n], else OPS_BAD_OFFSETS into *flag
+void launch_check_offsets(const int64_t* offsets, int groups, int64_t n, uint32_t* flag, hipStream_t s);
+
+// ---- grouped products ---------------------------------------------------------------------------
+enum { GP_FORWARD = 0, GP_DX = 1, GP_DA = 2 };
+
+struct GroupArgs {
+  const void* x;        // [n x k]
+  const void* a;        // [groups x m x k]
+  const void* dy;       // [n x m]
+  void* out;            // y [n x m], dx [n x k] or da [groups x m x k]
+  int64_t ldx, lddy, ldo;
+  const int64_t* offsets;
+  int groups;
+  int64_t n;
+  int k, m;             // in_dim, out_dim
+  const uint32_t* bad;  // the check's verdict, read by every workgroup
+  uint32_t* host_bad;   // receives it where it is not 0
+};
+
+// false: the grid would not fit
+bool launch_group_product(const GroupArgs& g, int type, int which, hipStream_t s);
+
+// ---- preference loss ----------------------------------------------------------------------------
+struct PrefArgs {
+  const void* logits;
+  int64_t ld;
+  const int32_t* labels;
+  const int64_t* offsets;
+  int pairs;
+  int64_t n;
+  int V;
+  const float* ref;
+  float beta, smoothing;
+  float* loss;
+  float* logp;
+  float* dlogp;          // written by the loss, read by its backward
+  float* stats;          // [n][2]
+  double* picked;        // workspace: each row's log probability (0 where it does not count)
+  void* dlogits;
+  int64_t lddl;
+  uint32_t* bad;
+  uint32_t* host_bad;
+};
+
+void launch_check_labels(const PrefArgs& p, hipStream_t s);
+void launch_preference_loss(const PrefArgs& p, int type, hipStream_t s);
+void launch_preference_backward(const PrefArgs& p, int type, hipStream_t s);
+
+// ---- clipping -----------------------------------------------------------------------------------
+constexpr int kClipBatch = 96;          // tensors a launch takes (its arguments hold their descriptors)
+constexpr int kClipBlock = 16384;       // values a workgroup takes
+
+struct ClipBatch {
+  const void* g[kClipBatch];
+  void* o[kClipBatch];
+  int64_t count[kClipBatch];
+  uint32_t first[kClipBatch + 1];       // first workgroup of each tensor; first[n]: their number
+  uint8_t type[kClipBatch];
+  int32_t n;
+};
+
+// the sums of squares of the batch's blocks into parts
+void launch_clip_squares(const ClipBatch& b, double* parts, hipStream_t s);
+// norm and factor from all parts: scale[0] = the factor; *host_norm = the norm
+void launch_clip_factor(const double* parts, int64_t n, double max_norm, double* scale, double* host_norm, hipStream_t s);
+void launch_clip_scale(const ClipBatch& b, const double* scale, hipStream_t s);

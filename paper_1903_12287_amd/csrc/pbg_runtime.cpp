@@ -378,6 +378,8 @@ void pbg_free(pbg_ctx* ctx) {
   if (ctx->check_ev) (void)hipEventDestroy(ctx->check_ev);
   if (ctx->edge_flag) (void)hipFree(ctx->edge_flag);
   if (ctx->edge_hflag) (void)hipHostFree(ctx->edge_hflag);
+  if (ctx->ops_ws) (void)hipFree(ctx->ops_ws);
+  if (ctx->ops_host) (void)hipHostFree(ctx->ops_host);
   for (hipEvent_t e : ctx->events) (void)hipEventDestroy(e);
   delete ctx;
 }

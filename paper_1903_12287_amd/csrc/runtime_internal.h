@@ -98,6 +98,11 @@ struct pbg_ctx {
   uint32_t* edge_hflag = nullptr;     // out of range, in page-locked memory; both 0 ...
   bool edge_dirty = false;            // ... unless a call ended without knowing so
   bool check_pending = false;
+  // workspace of the operators on a caller's own tensors (pbg_operators.cpp), and page-locked memory for the
+  // number that one of them hands back
+  void* ops_ws = nullptr;
+  size_t ops_ws_bytes = 0;
+  double* ops_host = nullptr;
   double* steploss_dev = nullptr;
   int64_t steploss_cap = 0;
   // the finalisation's loss partials of every step of a call, lossparts_pps

@@ -1,0 +1,184 @@
+"""Python binding of include/pbg_operators.h (argument marshalling only).
+
+The operators on a caller's own tensors: grouped matrix products, the preference loss and gradient clipping.  As in
+pbg.py every function has the name of its C entry point, checks dtypes, devices, shapes and layouts, passes raw
+pointers and raises pbg.PbgError when the call returns an error status.  Contexts come from pbg.pbg_bucket_init.
+"""
+
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import pbg
+
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+MAX_LD = 1 << 20       # PBG_OPS_MAX_LD
+MAX_DIM = 1 << 16      # PBG_OPS_MAX_DIM
+
+# every entry point the header declares
+EXPORTS = ("pbg_group_linear", "pbg_group_linear_backward", "pbg_preference_loss", "pbg_preference_loss_backward",
+           "pbg_clip_gradients")
+
+_ready = None
+
+
+def library() -> ctypes.CDLL:
+    """The library of pbg.py, with the signatures of this header's entry points."""
+    global _ready
+    if _ready is not None:
+        return _ready
+    L = pbg.library()
+    vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    f64, dp = ctypes.c_double, ctypes.POINTER(ctypes.c_double)
+    sig = {
+        "pbg_group_linear": [vp, i32, vp, i64, vp, vp, i32, i64, i32, i32, vp, i64],
+        "pbg_group_linear_backward": [vp, i32, vp, i64, vp, vp, i64, vp, i32, i64, i32, i32, vp, i64, vp],
+        "pbg_preference_loss": [vp, i32, vp, i64, vp, vp, i32, i64, i32, vp, f32, f32, vp, vp, vp, vp],
+        "pbg_preference_loss_backward": [vp, i32, vp, i64, vp, vp, i32, i64, i32, vp, vp, vp, i64],
+        "pbg_clip_gradients": [vp, i32, vp, vp, vp, vp, f64, dp],
+    }
+    for name, args in sig.items():
+        fn = getattr(L, name)
+        fn.argtypes = args
+        fn.restype = i32
+    _ready = L
+    return L
+
+
+def _check(ctx, status):
+    if status != 0:
+        msg = library().pbg_last_error(ctx)
+        raise pbg.PbgError(status, msg.decode() if msg else "")
+
+
+def _type(t, what):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what} must be a torch.Tensor")
+    if t.dtype not in TYPES:
+        raise TypeError(f"{what} must be float32, bfloat16 or float16, got {t.dtype}")
+    return t.dtype
+
+
+def _rows(t, dtype, shape, what):
+    """Pointer and row stride of a device matrix whose columns are consecutive."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what} must be a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.device.type != "cuda":
+        raise ValueError(f"{what} must be a device tensor")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {tuple(shape)}, got {tuple(t.shape)}")
+    n, width = shape
+    if width > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what} must have consecutive columns")
+    return (ctypes.c_void_p(t.data_ptr()) if t.numel() else None), (t.stride(0) if n > 1 else max(width, 1))
+
+
+def _vector(t, dtype, n, what, allow_none=False):
+    if t is not None and isinstance(t, torch.Tensor) and t.numel() != n:
+        raise ValueError(f"{what} must hold {n} values, got {t.numel()}")
+    return pbg._ptr(t, dtype, what, allow_none=allow_none)
+
+
+def _matrices(a, dtype, what):
+    if not isinstance(a, torch.Tensor) or a.dim() != 3:
+        raise ValueError(f"{what} must be [groups, out_dim, in_dim]")
+    return pbg._ptr(a, dtype, what)
+
+
+# ------------------------------------------------------------------ entry points
+def pbg_group_linear(ctx, x, a, offsets, y):
+    """x [n, in_dim], a [groups, out_dim, in_dim] contiguous, offsets int64 [groups + 1], y [n, out_dim] (written)."""
+    dt = _type(x, "x")
+    ap = _matrices(a, dt, "a")
+    if x.dim() != 2:
+        raise ValueError("x must be [n, in_dim]")
+    groups, m, k = a.shape
+    n = x.shape[0]
+    xp, ldx = _rows(x, dt, (n, k), "x")
+    yp, ldy = _rows(y, dt, (n, m), "y")
+    _check(ctx, library().pbg_group_linear(ctx, TYPES[dt], xp, ldx, ap,
+                                           _vector(offsets, torch.int64, groups + 1, "offsets"), groups, n, k, m, yp,
+                                           ldy))
+
+
+def pbg_group_linear_backward(ctx, x, a, offsets, dy, dx=None, da=None):
+    """dx [n, in_dim] and da [groups, out_dim, in_dim] are written; None: not wanted (x or a may then be None too)."""
+    dt = _type(dy, "dy")
+    if dy.dim() != 2:
+        raise ValueError("dy must be [n, out_dim]")
+    if a is None and da is None:
+        raise ValueError("a is needed for dx, da for the matrices' gradients: one of them is required")
+    n, m = dy.shape
+    ap = None if a is None else _matrices(a, dt, "a")
+    dap = None if da is None else _matrices(da, dt, "da")
+    groups, rows, k = (a if a is not None else da).shape
+    if rows != m or (a is not None and da is not None and a.shape != da.shape):
+        raise ValueError(f"a and da must be [groups, {m}, in_dim]")
+    xp, ldx = _rows(x, dt, (n, k), "x") if x is not None else (None, k)
+    dxp, lddx = _rows(dx, dt, (n, k), "dx") if dx is not None else (None, k)
+    dyp, lddy = _rows(dy, dt, (n, m), "dy")
+    if n and ((dx is not None and a is None) or (da is not None and x is None)):
+        raise ValueError("dx needs a, da needs x")
+    _check(ctx, library().pbg_group_linear_backward(
+        ctx, TYPES[dt], xp, ldx, ap, dyp, lddy, _vector(offsets, torch.int64, groups + 1, "offsets"), groups, n, k, m,
+        dxp, lddx, dap))
+
+
+def pbg_preference_loss(ctx, logits, labels, offsets, ref_logp, beta, smoothing, loss, logp, dlogp, row_stats):
+    """logits [n, candidates], labels int32 [n], offsets int64 [2 pairs + 1]; ref_logp float32 [2 pairs] or None.
+    Written: loss [pairs] (or None), logp [2 pairs], dlogp [2 pairs] (or None), row_stats [n, 2], all float32."""
+    dt = _type(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError("logits must be [n, candidates]")
+    n, cands = logits.shape
+    pairs = (offsets.numel() - 1) // 2
+    lp, ld = _rows(logits, dt, (n, cands), "logits")
+    f = torch.float32
+    _check(ctx, library().pbg_preference_loss(
+        ctx, TYPES[dt], lp, ld, _vector(labels, torch.int32, n, "labels"),
+        _vector(offsets, torch.int64, 2 * pairs + 1, "offsets"), pairs, n, cands,
+        _vector(ref_logp, f, 2 * pairs, "ref_logp", True), float(beta), float(smoothing),
+        _vector(loss, f, pairs, "loss", True), _vector(logp, f, 2 * pairs, "logp"),
+        _vector(dlogp, f, 2 * pairs, "dlogp", True), _vector(row_stats, f, 2 * n, "row_stats")))
+
+
+def pbg_preference_loss_backward(ctx, logits, labels, offsets, row_stats, dlogp, dlogits):
+    """dlogits [n, candidates] is written, and may be logits itself; dlogp float32 [2 pairs]."""
+    dt = _type(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError("logits must be [n, candidates]")
+    n, cands = logits.shape
+    pairs = (offsets.numel() - 1) // 2
+    lp, ld = _rows(logits, dt, (n, cands), "logits")
+    dp, lddl = _rows(dlogits, dt, (n, cands), "dlogits")
+    f = torch.float32
+    _check(ctx, library().pbg_preference_loss_backward(
+        ctx, TYPES[dt], lp, ld, _vector(labels, torch.int32, n, "labels"),
+        _vector(offsets, torch.int64, 2 * pairs + 1, "offsets"), pairs, n, cands,
+        _vector(row_stats, f, 2 * n, "row_stats"), _vector(dlogp, f, 2 * pairs, "dlogp"), dp, lddl))
+
+
+def pbg_clip_gradients(ctx, grads, max_norm, outs=None) -> float:
+    """grads: tensors of any shapes (contiguous; float32, bfloat16, float16 mixed); outs: tensors like them, or None to
+    scale in place.  Returns the joint norm before the scaling."""
+    n = len(grads)
+    if outs is not None and len(outs) != n:
+        raise ValueError("one output per gradient")
+    gp, op = (ctypes.c_void_p * max(n, 1))(), (ctypes.c_void_p * max(n, 1))()
+    counts, types = (ctypes.c_int64 * max(n, 1))(), (ctypes.c_int32 * max(n, 1))()
+    for i, g in enumerate(grads):
+        dt = _type(g, f"grads[{i}]")
+        gp[i] = pbg._ptr(g, dt, f"grads[{i}]")
+        counts[i], types[i] = g.numel(), TYPES[dt]
+        if outs is not None:
+            if isinstance(outs[i], torch.Tensor) and outs[i].shape != g.shape:
+                raise ValueError(f"outs[{i}] must be {tuple(g.shape)}, got {tuple(outs[i].shape)}")
+            op[i] = pbg._ptr(outs[i], dt, f"outs[{i}]")
+    norm = ctypes.c_double(0.0)
+    _check(ctx, library().pbg_clip_gradients(ctx, n, types, counts, gp, None if outs is None else op, float(max_norm),
+                                             ctypes.byref(norm)))
+    return norm.value
