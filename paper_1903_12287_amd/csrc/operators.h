@@ -19,21 +19,33 @@ void launch_check_offsets(const int64_t* offsets, int groups, int64_t n, uint32_
 enum { GP_FORWARD = 0, GP_DX = 1, GP_DA = 2 };
 
 struct GroupArgs {
-  const void* x;        // [n x k]
-  const void* a;        // [groups x m x k]
-  const void* dy;       // [n x m]
+  const void* x;        // [n x kd]
+  const void* a;        // [groups x a_group], rows of lda
+  const void* dy;       // [n x md]
   void* out;            // y [n x m], dx [n x k] or da [groups x m x k]
-  int64_t ldx, lddy, ldo;
+  int64_t ldx, lda, lddy, ldo;
+  int64_t a_group;      // values from a matrix to the next
   const int64_t* offsets;
   int groups;
   int64_t n;
   int k, m;             // in_dim, out_dim
+  int kd, md;           // widths that the operands hold: rounded up to 16 bytes where they were packed, zeros behind
   const uint32_t* bad;  // the check's verdict, read by every workgroup
   uint32_t* host_bad;   // receives it where it is not 0
 };
 
+struct GroupPlan {
+  int da_shift;            // da: rows of a slot, 2^da_shift
+  int64_t partial_slots;   // slots of partial sums, m k floats each (0: no group is longer than a slot)
+  float* partial;
+};
+
+void plan_group_da(int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p);
+// up to three operands into rows of wp values, a multiple of 16 bytes, zeros behind `width`
+void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,
+                       const int64_t* rows, const int* width, const int* wp, hipStream_t s);
 // false: the grid would not fit
-bool launch_group_product(const GroupArgs& g, int type, int which, hipStream_t s);
+bool launch_group_product(const GroupArgs& g, int type, int which, const GroupPlan& p, hipStream_t s);
 
 // ---- preference loss ----------------------------------------------------------------------------
 struct PrefArgs {

@@ -1,88 +1,188 @@
 // Products with one matrix per group of rows (include/pbg_operators.h, pbg_group_linear):
-//   forward  y[t, :]  = A_g x[t, :]            over in_dim
-//   dx       dx[t, :] = A_g^T dy[t, :]         over out_dim
+//   forward  y[t, :]  = A_g x[t, :]                over in_dim
+//   dx       dx[t, :] = A_g^T dy[t, :]             over out_dim
 //   da       dA_g     = sum_t dy[t, :] x[t, :]^T   over the group's rows
-#include "operators_device.h"
+// The host does not know the groups' sizes: a workgroup finds its group and rows from the offsets alone
+// (group_of_slot), so a call needs neither a table nor a wait before its product.
+#include <algorithm>
+
+#include "operators_tile.h"
 
 namespace {
 
-constexpr int kTile = 64;     // rows and columns of a tile
-constexpr int kShift = 6;
-constexpr int kDepth = 16;
+using tile::KC;
+using tile::KR;
 
-// One 64 x 64 tile of a product C = P Q^T, P[i][k] at p + i pi + k pk and Q[j][k] at q + j qi + k qk (elements).
-template <int TYPE>
-__device__ __forceinline__ void tile_product(const typename Elem<TYPE>::T* p, int64_t pi, int64_t pk, int rows,
-                                             const typename Elem<TYPE>::T* q, int64_t qi, int64_t qk, int cols,
-                                             int64_t depth, typename Elem<TYPE>::T* c, int64_t ldc) {
-  typedef typename Elem<TYPE>::T T;
-  __shared__ float ps[kDepth][kTile + 1], qs[kDepth][kTile + 1];
-  const int tid = threadIdx.x, ti = tid >> 4, tj = tid & 15;
-  float acc[4][4] = {};
-  for (int64_t k0 = 0; k0 < depth; k0 += kDepth) {
-    __syncthreads();
-    for (int f = tid; f < kDepth * kTile; f += 256) {
-      const int i = f / kDepth, k = f % kDepth;
-      const bool in = k0 + k < depth;
-      ps[k][i] = in && i < rows ? (float)p[i * pi + (k0 + k) * pk] : 0.0f;
-      qs[k][i] = in && i < cols ? (float)q[i * qi + (k0 + k) * qk] : 0.0f;
-    }
-    __syncthreads();
-    for (int k = 0; k < kDepth; ++k) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[u][v] += ps[k][ti + 16 * u] * qs[k][tj + 16 * v];
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < 4; ++u)
-#pragma unroll
-    for (int v = 0; v < 4; ++v)
-      if (ti + 16 * u < rows && tj + 16 * v < cols) c[(ti + 16 * u) * ldc + tj + 16 * v] = (T)acc[u][v];
-}
+struct Launch {
+  int shift;              // rows of a slot: 2^shift
+  int row_tiles, col_tiles;   // da: tiles of one matrix; else row_tiles is 1
+  uint32_t blocks;
+  bool vec;               // rows of the output start at multiples of four values
+  float* partial;         // da: partial sums of the groups of several slots
+};
 
-template <int TYPE, int WHICH>
-__global__ __launch_bounds__(256) void group_rows_kernel(GroupArgs g, int col_tiles) {
-  typedef typename Elem<TYPE>::T T;
+// y and dx: one slot of a group's rows, one tile of the output's columns
+template <int TYPE, int WHICH, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void group_rows_kernel(GroupArgs g, Launch L) {
+  typedef tile::Tile<TYPE, KC, WHICH == GP_FORWARD ? KC : KR, BM, BN, WM, WN> Tl;
+  constexpr int ES = TYPE == OT_F32 ? 4 : 2;
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
   if (!args_good(g.bad, g.host_bad)) return;
-  const int64_t slot = blockIdx.x / col_tiles;
-  const int j0 = (int)(blockIdx.x % col_tiles) * kTile;
-  const int grp = group_of_slot(g.offsets, g.groups, kShift, slot);
+  const uint32_t at = tile::xcd_place(blockIdx.x, L.blocks);
+  const int64_t slot = at / L.col_tiles;
+  const int j0 = (int)(at % L.col_tiles) * BN;
+  const int grp = group_of_slot(g.offsets, g.groups, L.shift, slot);
   if (grp < 0) return;
-  const int64_t r0 = g.offsets[grp] + ((slot - first_slot(g.offsets, grp, kShift)) << kShift);
-  const int rows = (int)min((int64_t)kTile, g.offsets[grp + 1] - r0);
+  const int64_t r0 = g.offsets[grp] + ((slot - first_slot(g.offsets, grp, L.shift)) << L.shift);
+  const int rows = (int)min((int64_t)BM, g.offsets[grp + 1] - r0);
   if (rows <= 0) return;
-  const T* a = (const T*)g.a + (int64_t)grp * g.m * g.k;
-  T* out = (T*)g.out + r0 * g.ldo + j0;
+  const char* a = (const char*)g.a + grp * g.a_group * ES;
+  v4f acc[Tl::IB][Tl::JB];
+  const int width = WHICH == GP_FORWARD ? g.m : g.k;
   if (WHICH == GP_FORWARD)
-    tile_product<TYPE>((const T*)g.x + r0 * g.ldx, g.ldx, 1, rows, a + (int64_t)j0 * g.k, g.k, 1, g.m - j0, g.k, out, g.ldo);
+    Tl::run(lds, (const char*)g.x + r0 * g.ldx * ES, g.ldx, rows, a + (int64_t)j0 * g.lda * ES, g.lda, g.m - j0, g.kd, acc);
   else
-    tile_product<TYPE>((const T*)g.dy + r0 * g.lddy, g.lddy, 1, rows, a + j0, 1, g.k, g.k - j0, g.m, out, g.ldo);
+    Tl::run(lds, (const char*)g.dy + r0 * g.lddy * ES, g.lddy, rows, a + (int64_t)j0 * ES, g.lda, g.kd - j0, g.m, acc);
+  Tl::template store<TYPE>(acc, (char*)g.out + (r0 * g.ldo + j0) * ES, g.ldo, rows, width - j0, L.vec);
+}
+
+// da: one slot of a group's rows, one tile of its matrix.  A group of one slot is stored; the slots of a longer one
+// leave float32 sums, which group_join_kernel adds in their order.  Group g's slots of partial sums start at
+// floor(2 offsets[g] / 2^shift): a group of L > 2^shift rows has at least ceil(L / 2^shift) of them.
+__device__ __forceinline__ int64_t first_partial(const int64_t* offsets, int g, int shift) {
+  return (2 * offsets[g]) >> shift;
+}
+
+template <int TYPE, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Launch L) {
+  typedef tile::Tile<TYPE, KR, KR, BM, BN, WM, WN> Tl;
+  constexpr int ES = TYPE == OT_F32 ? 4 : 2;
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  if (!args_good(g.bad, g.host_bad)) return;
+  const uint32_t at = tile::xcd_place(blockIdx.x, L.blocks);
+  const int tiles = L.row_tiles * L.col_tiles;
+  const int64_t slot = at / tiles;
+  const int t = (int)(at % tiles);
+  const int i0 = t / L.col_tiles * BM, j0 = t % L.col_tiles * BN;
+  const int grp = group_of_slot(g.offsets, g.groups, L.shift, slot);
+  if (grp < 0) return;
+  const int64_t first = g.offsets[grp], last = g.offsets[grp + 1];
+  const int64_t part = slot - first_slot(g.offsets, grp, L.shift);
+  const int64_t r0 = first + (part << L.shift);
+  if (part > 0 && r0 >= last) return;   // slot 0 of an empty group stores zeros
+  const int64_t depth = min((int64_t)1 << L.shift, last - r0);
+  v4f acc[Tl::IB][Tl::JB];
+  Tl::run(lds, (const char*)g.dy + (r0 * g.lddy + i0) * ES, g.lddy, g.md - i0, (const char*)g.x + (r0 * g.ldx + j0) * ES,
+          g.ldx, g.kd - j0, depth, acc);
+  const int rows = min(BM, g.m - i0), cols = g.k - j0;
+  if (last - first <= (int64_t)1 << L.shift) {
+    Tl::template store<TYPE>(acc, (char*)g.out + (((int64_t)grp * g.m + i0) * g.k + j0) * ES, g.k, rows, cols, L.vec);
+  } else {
+    float* p = L.partial + (first_partial(g.offsets, grp, L.shift) + part) * g.m * g.k;
+    Tl::template store<OT_F32>(acc, p + (int64_t)i0 * g.k + j0, g.k, rows, cols, (g.k & 3) == 0);
+  }
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(256) void group_da_kernel(GroupArgs g, int m_tiles, int k_tiles) {
+__global__ __launch_bounds__(256) void group_join_kernel(GroupArgs g, Launch L) {
   typedef typename Elem<TYPE>::T T;
   if (!args_good(g.bad, g.host_bad)) return;
-  const int grp = blockIdx.x / (m_tiles * k_tiles), tile = blockIdx.x % (m_tiles * k_tiles);
-  const int i0 = tile / k_tiles * kTile, j0 = tile % k_tiles * kTile;
-  const int64_t r0 = g.offsets[grp], depth = g.offsets[grp + 1] - r0;
-  tile_product<TYPE>((const T*)g.dy + r0 * g.lddy + i0, 1, g.lddy, g.m - i0, (const T*)g.x + r0 * g.ldx + j0, 1, g.ldx,
-                     g.k - j0, depth, (T*)g.out + ((int64_t)grp * g.m + i0) * g.k + j0, g.k);
+  // first_partial(grp) <= slot; a group of several slots holds two partial slots at least, so at its first one it is
+  // the last group that starts there or before
+  const int64_t slot = blockIdx.y;
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = g.groups;
+  while (true) {
+    const int step = (hi - lo + 63) >> 6;
+    const int q = lo + lane * step;
+    const int c = __popcll(__ballot(q < hi && first_partial(g.offsets, q, L.shift) <= slot));
+    if (c == 0) return;
+    lo += (c - 1) * step;
+    if (step == 1) break;
+    hi = min(hi, lo + step);
+  }
+  const int grp = __builtin_amdgcn_readfirstlane(lo);
+  const int64_t rows = g.offsets[grp + 1] - g.offsets[grp];
+  if (first_partial(g.offsets, grp, L.shift) != slot || rows <= (int64_t)1 << L.shift) return;
+  const int parts = (int)((rows + ((int64_t)1 << L.shift) - 1) >> L.shift);
+  const int64_t mk = (int64_t)g.m * g.k;
+  const float* p = L.partial + slot * mk;
+  T* out = (T*)g.out + grp * mk;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < mk; e += (int64_t)gridDim.x * 256) {
+    float s = p[e];
+    for (int i = 1; i < parts; ++i) s += p[i * mk + e];
+    out[e] = (T)s;
+  }
+}
+
+// Copies rows of `width` values into rows of `wp` >= width, a multiple of 16 bytes, with zeros behind them.
+struct PackArgs {
+  const void* src[3];
+  void* dst[3];
+  int64_t ld[3], rows[3];
+  int width[3], wp[3];
+  uint32_t first[4];   // first workgroup of each
+};
+
+constexpr int kPackRows = 16;
+
+template <int TYPE>
+__global__ __launch_bounds__(256) void group_pack_kernel(PackArgs a) {
+  typedef typename Elem<TYPE>::T T;
+  const int w = blockIdx.x >= a.first[2] ? 2 : (blockIdx.x >= a.first[1] ? 1 : 0);
+  const int64_t r0 = (int64_t)(blockIdx.x - a.first[w]) * kPackRows;
+  const int64_t r1 = min(a.rows[w], r0 + kPackRows);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  for (int64_t r = r0 + wave; r < r1; r += 4) {
+    const T* s = (const T*)a.src[w] + r * a.ld[w];
+    T* d = (T*)a.dst[w] + r * a.wp[w];
+    for (int c = lane; c < a.wp[w]; c += 64) d[c] = c < a.width[w] ? s[c] : (T)0.0f;
+  }
+}
+
+// ---- what is launched ------------------------------------------------------------------------------
+int64_t tiles_of(int64_t v, int b) { return (v + b - 1) / b; }
+
+template <int TYPE, int WHICH, int BM, int BN, int WM, int WN>
+bool launch_rows(const GroupArgs& g, Launch L, hipStream_t s) {
+  L.shift = __builtin_ctz(BM);
+  L.row_tiles = 1;
+  L.col_tiles = (int)tiles_of(WHICH == GP_FORWARD ? g.m : g.k, BN);
+  const int64_t blocks = ((g.n >> L.shift) + g.groups) * L.col_tiles;
+  if (blocks * 64 * WM * WN >= 1ll << 32) return false;
+  L.blocks = (uint32_t)blocks;
+  group_rows_kernel<TYPE, WHICH, BM, BN, WM, WN><<<L.blocks, 64 * WM * WN, 0, s>>>(g, L);
+  return true;
+}
+
+template <int TYPE, int BM, int BN, int WM, int WN>
+bool launch_da(const GroupArgs& g, Launch L, hipStream_t s) {
+  L.row_tiles = (int)tiles_of(g.m, BM);
+  L.col_tiles = (int)tiles_of(g.k, BN);
+  const int64_t blocks = ((g.n >> L.shift) + g.groups) * L.row_tiles * L.col_tiles;
+  if (blocks * 64 * WM * WN >= 1ll << 32) return false;
+  L.blocks = (uint32_t)blocks;
+  group_da_kernel<TYPE, BM, BN, WM, WN><<<L.blocks, 64 * WM * WN, 0, s>>>(g, L);
+  return true;
 }
 
 template <int TYPE>
-bool launch_typed(const GroupArgs& g, int which, hipStream_t s) {
-  const int mt = (g.m + kTile - 1) / kTile, kt = (g.k + kTile - 1) / kTile;
-  const int64_t slots = (g.n >> kShift) + g.groups;
-  const int64_t blocks = which == GP_DA ? (int64_t)g.groups * mt * kt : slots * (which == GP_FORWARD ? mt : kt);
-  if (blocks > (1ll << 32) / 256 - 1) return false;
-  const unsigned nb = (unsigned)blocks;
-  if (which == GP_FORWARD) group_rows_kernel<TYPE, GP_FORWARD><<<nb, 256, 0, s>>>(g, mt);
-  else if (which == GP_DX) group_rows_kernel<TYPE, GP_DX><<<nb, 256, 0, s>>>(g, kt);
-  else group_da_kernel<TYPE><<<nb, 256, 0, s>>>(g, mt, kt);
-  return true;
+bool launch_typed(const GroupArgs& g, int which, const GroupPlan& p, hipStream_t s) {
+  Launch L{};
+  L.vec = g.ldo % 4 == 0 && ((uintptr_t)g.out & (TYPE == OT_F32 ? 15 : 7)) == 0;
+  if (which == GP_DA) {
+    L.shift = p.da_shift;
+    L.partial = p.partial;
+    if (!launch_da<TYPE, 128, 128, 2, 2>(g, L, s)) return false;
+    if (p.partial_slots > 0) {
+      const int64_t mk = (int64_t)g.m * g.k;
+      const dim3 grid((unsigned)std::min<int64_t>(tiles_of(mk, 1024), 1024), (unsigned)p.partial_slots);
+      group_join_kernel<TYPE><<<grid, 256, 0, s>>>(g, L);
+    }
+    return true;
+  }
+  if (which == GP_FORWARD) return launch_rows<TYPE, GP_FORWARD, 128, 128, 2, 2>(g, L, s);
+  return launch_rows<TYPE, GP_DX, 128, 128, 2, 2>(g, L, s);
 }
 
 __global__ __launch_bounds__(256) void check_offsets_kernel(const int64_t* offsets, int groups, int64_t n,
@@ -102,10 +202,50 @@ void launch_check_offsets(const int64_t* offsets, int groups, int64_t n, uint32_
   check_offsets_kernel<<<blocks < 1024 ? blocks : 1024, 256, 0, s>>>(offsets, groups, n, flag);
 }
 
-bool launch_group_product(const GroupArgs& g, int type, int which, hipStream_t s) {
+void plan_group_da(int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p) {
+  // Rows of a slot: enough slots for a few workgroups on each of the 256 compute units, where the matrices' tiles
+  // alone are not; with tiles enough, only groups of four times the average and more are cut.
+  const int64_t tiles = tiles_of(m, 128) * tiles_of(k, 128);
+  int64_t rows = std::max<int64_t>(256, n * tiles / 1024);
+  if (groups * tiles >= 512) rows = std::max(rows, 4 * n / groups);
+  int shift = 8;
+  while (shift < 31 && ((int64_t)1 << shift) < rows) ++shift;
+  // the partial sums stay below 512 MB
+  while (shift < 31 && ((2 * n) >> shift) * m * k * 4 > (512ll << 20)) ++shift;
+  p->da_shift = shift;
+  p->partial_slots = n > (int64_t)1 << shift ? (2 * n) >> shift : 0;
+  // a grid has 65,535 slots
+  while (p->partial_slots > 65535) {
+    p->da_shift = ++shift;
+    p->partial_slots = n > (int64_t)1 << shift ? (2 * n) >> shift : 0;
+  }
+}
+
+void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,
+                       const int64_t* rows, const int* width, const int* wp, hipStream_t s) {
+  PackArgs a{};
+  uint32_t at = 0;
+  for (int i = 0; i < 3; ++i) {
+    a.first[i] = at;
+    if (i >= count) continue;
+    a.src[i] = src[i];
+    a.dst[i] = dst[i];
+    a.ld[i] = ld[i];
+    a.rows[i] = rows[i];
+    a.width[i] = width[i];
+    a.wp[i] = wp[i];
+    at += (uint32_t)tiles_of(rows[i], kPackRows);
+  }
+  if (!at) return;
+  if (type == OT_F32) group_pack_kernel<OT_F32><<<at, 256, 0, s>>>(a);
+  else if (type == OT_BF16) group_pack_kernel<OT_BF16><<<at, 256, 0, s>>>(a);
+  else group_pack_kernel<OT_F16><<<at, 256, 0, s>>>(a);
+}
+
+bool launch_group_product(const GroupArgs& g, int type, int which, const GroupPlan& p, hipStream_t s) {
   switch (type) {
-    case OT_F32: return launch_typed<OT_F32>(g, which, s);
-    case OT_BF16: return launch_typed<OT_BF16>(g, which, s);
-    default: return launch_typed<OT_F16>(g, which, s);
+    case OT_F32: return launch_typed<OT_F32>(g, which, p, s);
+    case OT_BF16: return launch_typed<OT_BF16>(g, which, p, s);
+    default: return launch_typed<OT_F16>(g, which, p, s);
   }
 }

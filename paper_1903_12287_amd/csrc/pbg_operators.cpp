@@ -86,6 +86,45 @@ bool aligned(const void* p, int es) { return ((uintptr_t)p & (uintptr_t)(es - 1)
 
 bool bad_ld(int64_t ld, int64_t width) { return ld < width || ld > PBG_OPS_MAX_LD; }
 
+// The operands of a grouped product as the matrix kernels read them: rows at multiples of 16 bytes, whole 16 bytes
+// of values.  Others are copied into the workspace (behind `front` bytes of it), zeros behind their rows.
+struct Operands {
+  int64_t es, ev;
+  int count = 0;
+  const void* src[3];
+  void* dst[3];
+  int64_t ld[3], rows[3];
+  int width[3], wp[3];
+  size_t bytes = 0;
+  size_t at[3];
+  const void** p[3];
+  int64_t* out_ld[3];
+  explicit Operands(int type) : es(type_bytes(type)), ev(16 / type_bytes(type)) {}
+  int padded(int w) const { return (int)((w + ev - 1) / ev * ev); }
+  // *ptr (rows of *row_ld) is used as it is or replaced by its copy
+  void add(const void** ptr, int64_t* row_ld, int64_t n, int w) {
+    if (!*ptr || n <= 0) return;
+    if (((uintptr_t)*ptr & 15) == 0 && *row_ld % ev == 0 && w % ev == 0) return;
+    src[count] = *ptr;
+    ld[count] = *row_ld;
+    rows[count] = n;
+    width[count] = w;
+    wp[count] = padded(w);
+    at[count] = bytes;
+    bytes += ((size_t)n * wp[count] * es + 255) & ~(size_t)255;
+    p[count] = ptr;
+    out_ld[count] = row_ld;
+    ++count;
+  }
+  void place(char* ws) {
+    for (int i = 0; i < count; ++i) {
+      dst[i] = ws + at[i];
+      *p[i] = dst[i];
+      *out_ld[i] = wp[i];
+    }
+  }
+};
+
 pbg_status check_group(pbg_ctx* ctx, int32_t dtype, const int64_t* offsets, int32_t groups, int64_t n, int32_t in_dim,
                        int32_t out_dim) {
   if (dtype < PBG_TYPE_F32 || dtype > PBG_TYPE_F16) return set_err(ctx, PBG_ERR_INVALID_ARG, "unknown type %d", dtype);
@@ -118,12 +157,24 @@ extern "C" pbg_status pbg_group_linear(pbg_ctx* ctx, int32_t dtype, const void* 
     return set_err(ctx, PBG_ERR_INVALID_ARG, "y overlaps an input");
   st = ensure_edge_flags(ctx);
   if (st != PBG_OK) return st;
+  GroupArgs g{x, a, nullptr, y, ldx, in_dim, 0, ldy, 0, offsets, groups, n, in_dim, out_dim, in_dim, out_dim,
+              ctx->edge_flag, ctx->edge_hflag};
+  Operands ops(dtype);
+  if (n > 0) {
+    ops.add(&g.x, &g.ldx, n, in_dim);
+    ops.add(&g.a, &g.lda, (int64_t)groups * out_dim, in_dim);
+  }
+  st = workspace(ctx, ops.bytes);
+  if (st != PBG_OK) return st;
+  ops.place((char*)ctx->ops_ws);
+  g.kd = ops.padded(in_dim);
+  g.a_group = (int64_t)out_dim * g.lda;
   ctx->edge_dirty = true;
   launch_check_offsets(offsets, groups, n, ctx->edge_flag, ctx->cs);
+  launch_group_pack(dtype, ops.count, ops.src, ops.dst, ops.ld, ops.rows, ops.width, ops.wp, ctx->cs);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) {
-    const GroupArgs g{x, a, nullptr, y, ldx, 0, ldy, offsets, groups, n, in_dim, out_dim, ctx->edge_flag, ctx->edge_hflag};
-    if (!launch_group_product(g, dtype, GP_FORWARD, ctx->cs)) {
+    if (!launch_group_product(g, dtype, GP_FORWARD, GroupPlan{}, ctx->cs)) {
       (void)hipStreamSynchronize(ctx->cs);
       return set_err(ctx, PBG_ERR_UNSUPPORTED, "more tiles than a launch holds");
     }
@@ -155,18 +206,38 @@ extern "C" pbg_status pbg_group_linear_backward(pbg_ctx* ctx, int32_t dtype, con
   if (overlap(rdx, rda)) return set_err(ctx, PBG_ERR_INVALID_ARG, "dx and da overlap");
   st = ensure_edge_flags(ctx);
   if (st != PBG_OK) return st;
+  GroupArgs g{x, a, dy, nullptr, ldx, in_dim, lddy, 0, 0, offsets, groups, n, in_dim, out_dim, in_dim, out_dim,
+              ctx->edge_flag, ctx->edge_hflag};
+  Operands ops(dtype);
+  GroupPlan plan{};
+  if (n > 0) {
+    ops.add(&g.dy, &g.lddy, n, out_dim);
+    if (da) ops.add(&g.x, &g.ldx, n, in_dim);
+    if (dx) ops.add(&g.a, &g.lda, gm, in_dim);
+  }
+  if (da) plan_group_da(n, groups, out_dim, in_dim, &plan);
+  st = workspace(ctx, ops.bytes + (size_t)plan.partial_slots * out_dim * in_dim * 4);
+  if (st != PBG_OK) return st;
+  ops.place((char*)ctx->ops_ws);
+  plan.partial = (float*)((char*)ctx->ops_ws + ops.bytes);
+  g.kd = ops.padded(in_dim);
+  g.md = ops.padded(out_dim);
+  g.a_group = (int64_t)out_dim * g.lda;
   ctx->edge_dirty = true;
   launch_check_offsets(offsets, groups, n, ctx->edge_flag, ctx->cs);
+  launch_group_pack(dtype, ops.count, ops.src, ops.dst, ops.ld, ops.rows, ops.width, ops.wp, ctx->cs);
   hipError_t e = hipGetLastError();
   bool fits = true;
   if (e == hipSuccess && dx) {
-    const GroupArgs g{x, a, dy, dx, ldx, lddy, lddx, offsets, groups, n, in_dim, out_dim, ctx->edge_flag, ctx->edge_hflag};
-    fits = launch_group_product(g, dtype, GP_DX, ctx->cs);
+    g.out = dx;
+    g.ldo = lddx;
+    fits = launch_group_product(g, dtype, GP_DX, plan, ctx->cs);
     e = hipGetLastError();
   }
   if (e == hipSuccess && fits && da) {
-    const GroupArgs g{x, a, dy, da, ldx, lddy, in_dim, offsets, groups, n, in_dim, out_dim, ctx->edge_flag, ctx->edge_hflag};
-    fits = launch_group_product(g, dtype, GP_DA, ctx->cs);
+    g.out = da;
+    g.ldo = in_dim;
+    fits = launch_group_product(g, dtype, GP_DA, plan, ctx->cs);
     e = hipGetLastError();
   }
   if (!fits) {
