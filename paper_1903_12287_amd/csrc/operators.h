@@ -35,12 +35,13 @@ struct GroupArgs {
 };
 
 struct GroupPlan {
+  bool da_wide;            // da: tiles of 256 x 256
   int da_shift;            // da: rows of a slot, 2^da_shift
   int64_t partial_slots;   // slots of partial sums, m k floats each (0: no group is longer than a slot)
   float* partial;
 };
 
-void plan_group_da(int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p);
+void plan_group_da(int type, int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p);
 // up to three operands into rows of wp values, a multiple of 16 bytes, zeros behind `width`
 void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,
                        const int64_t* rows, const int* width, const int* wp, hipStream_t s);

@@ -83,14 +83,18 @@ __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Lau
   }
 }
 
+// Adds a group's partial sums: 64 elements a workgroup, each of its four waves a quarter of the slots in their order,
+// then the waves in theirs.  (One thread an element over all slots: 65 us for 78 slots of 100 x 100, loads one behind
+// the other.)
 template <int TYPE>
 __global__ __launch_bounds__(256) void group_join_kernel(GroupArgs g, Launch L) {
   typedef typename Elem<TYPE>::T T;
+  __shared__ float sums[4][64];
   if (!args_good(g.bad, g.host_bad)) return;
   // first_partial(grp) <= slot; a group of several slots holds two partial slots at least, so at its first one it is
   // the last group that starts there or before
   const int64_t slot = blockIdx.y;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   int lo = 0, hi = g.groups;
   while (true) {
     const int step = (hi - lo + 63) >> 6;
@@ -105,13 +109,26 @@ __global__ __launch_bounds__(256) void group_join_kernel(GroupArgs g, Launch L) 
   const int64_t rows = g.offsets[grp + 1] - g.offsets[grp];
   if (first_partial(g.offsets, grp, L.shift) != slot || rows <= (int64_t)1 << L.shift) return;
   const int parts = (int)((rows + ((int64_t)1 << L.shift) - 1) >> L.shift);
+  const int per = (parts + 3) >> 2, i0 = w * per, i1 = min(parts, i0 + per);
   const int64_t mk = (int64_t)g.m * g.k;
   const float* p = L.partial + slot * mk;
   T* out = (T*)g.out + grp * mk;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < mk; e += (int64_t)gridDim.x * 256) {
-    float s = p[e];
-    for (int i = 1; i < parts; ++i) s += p[i * mk + e];
-    out[e] = (T)s;
+  for (int64_t e0 = (int64_t)blockIdx.x * 64; e0 < mk; e0 += (int64_t)gridDim.x * 64) {
+    const int64_t e = min(e0 + lane, mk - 1);
+    float s = 0.0f;
+    int i = i0;
+    for (; i + 8 <= i1; i += 8) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = p[(i + u) * mk + e];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
+    for (; i < i1; ++i) s += p[i * mk + e];
+    sums[w][lane] = s;
+    __syncthreads();
+    if (w == 0 && e0 + lane < mk) out[e] = (T)(((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane]);
+    __syncthreads();
   }
 }
 
@@ -166,6 +183,18 @@ bool launch_da(const GroupArgs& g, Launch L, hipStream_t s) {
   return true;
 }
 
+template <int TYPE, int WHICH>
+bool launch_rows_by_size(const GroupArgs& g, const Launch& L, hipStream_t s) {
+  const int64_t cols = WHICH == GP_FORWARD ? g.m : g.k;
+  const int64_t average = g.n / g.groups;
+  if constexpr (TYPE != OT_F32) {
+    if (average >= 256 && g.n / 256 * tiles_of(cols, 256) >= 256)
+      return launch_rows<TYPE, WHICH, 256, 256, 2, 4>(g, L, s);
+  }
+  if (average >= 64) return launch_rows<TYPE, WHICH, 128, 128, 2, 2>(g, L, s);
+  return launch_rows<TYPE, WHICH, 32, 128, 1, 4>(g, L, s);
+}
+
 template <int TYPE>
 bool launch_typed(const GroupArgs& g, int which, const GroupPlan& p, hipStream_t s) {
   Launch L{};
@@ -173,16 +202,20 @@ bool launch_typed(const GroupArgs& g, int which, const GroupPlan& p, hipStream_t
   if (which == GP_DA) {
     L.shift = p.da_shift;
     L.partial = p.partial;
-    if (!launch_da<TYPE, 128, 128, 2, 2>(g, L, s)) return false;
+    if constexpr (TYPE != OT_F32) {
+      if (p.da_wide ? !launch_da<TYPE, 256, 256, 2, 4>(g, L, s) : !launch_da<TYPE, 128, 128, 2, 2>(g, L, s)) return false;
+    } else {
+      if (!launch_da<TYPE, 128, 128, 2, 2>(g, L, s)) return false;
+    }
     if (p.partial_slots > 0) {
       const int64_t mk = (int64_t)g.m * g.k;
-      const dim3 grid((unsigned)std::min<int64_t>(tiles_of(mk, 1024), 1024), (unsigned)p.partial_slots);
+      const dim3 grid((unsigned)std::min<int64_t>(tiles_of(mk, 64), 4096), (unsigned)p.partial_slots);
       group_join_kernel<TYPE><<<grid, 256, 0, s>>>(g, L);
     }
     return true;
   }
-  if (which == GP_FORWARD) return launch_rows<TYPE, GP_FORWARD, 128, 128, 2, 2>(g, L, s);
-  return launch_rows<TYPE, GP_DX, 128, 128, 2, 2>(g, L, s);
+  if (which == GP_FORWARD) return launch_rows_by_size<TYPE, GP_FORWARD>(g, L, s);
+  return launch_rows_by_size<TYPE, GP_DX>(g, L, s);
 }
 
 __global__ __launch_bounds__(256) void check_offsets_kernel(const int64_t* offsets, int groups, int64_t n,
@@ -202,10 +235,12 @@ void launch_check_offsets(const int64_t* offsets, int groups, int64_t n, uint32_
   check_offsets_kernel<<<blocks < 1024 ? blocks : 1024, 256, 0, s>>>(offsets, groups, n, flag);
 }
 
-void plan_group_da(int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p) {
+void plan_group_da(int type, int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p) {
   // Rows of a slot: enough slots for a few workgroups on each of the 256 compute units, where the matrices' tiles
   // alone are not; with tiles enough, only groups of four times the average and more are cut.
-  const int64_t tiles = tiles_of(m, 128) * tiles_of(k, 128);
+  p->da_wide = type != OT_F32 && groups * tiles_of(m, 256) * tiles_of(k, 256) >= 256 && n / groups >= 2048;
+  const int b = p->da_wide ? 256 : 128;
+  const int64_t tiles = tiles_of(m, b) * tiles_of(k, b);
   int64_t rows = std::max<int64_t>(256, n * tiles / 1024);
   if (groups * tiles >= 512) rows = std::max(rows, 4 * n / groups);
   int shift = 8;

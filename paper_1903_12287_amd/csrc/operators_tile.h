@@ -153,29 +153,61 @@ struct Tile {
     if (nk == 0) return;
     op.fetch(lds, 0);
     oq.fetch(lds + P::BYTES, 0);
+    typename Mfma<TYPE>::Frag fp[2][IB], fq[2][JB];
+    auto read = [&](const char* stage, int s) {
+#pragma unroll
+      for (int j = 0; j < JB; ++j) fq[s][j] = Q::read(stage + P::BYTES, wn * JB + j, s, lane);
+#pragma unroll
+      for (int i = 0; i < IB; ++i) fp[s][i] = P::read(stage, wm * IB + i, s, lane);
+    };
+    auto multiply = [&](int s) {
+#pragma unroll
+      for (int i = 0; i < IB; ++i)
+#pragma unroll
+        for (int j = 0; j < JB; ++j) acc[i][j] = Mfma<TYPE>::mul(fq[s][j], fp[s][i], acc[i][j]);
+    };
+    pieces::wait_loads();      // this wave's part of the slice has landed,
+    pieces::lds_barrier();     // and everyone's
+    read(lds, 0);
+    op.fetch(lds + STAGE, 1);
+    oq.fetch(lds + STAGE + P::BYTES, 1);
+    // Half a slice is multiplied while the next half is read and the slice behind it fetched: one barrier a slice.
+    // The last two rounds fetch past the operands, which moves zeros, so that a round is one block of code.
     for (int kt = 0; kt < nk; ++kt) {
       char* now = lds + (kt & 1) * STAGE;
       char* next = lds + (~kt & 1) * STAGE;
-      pieces::wait_loads();      // this wave's part of the slice has landed,
-      pieces::lds_barrier();     // everyone's has, and the other stage has been read
-      typename Mfma<TYPE>::Frag fp[2][IB], fq[2][JB];
+      read(now, 1);
+      multiply(0);
+      interleave<0>();
+      __builtin_amdgcn_sched_barrier(0);   // the products stay ahead of the wait
+      pieces::wait_loads();    // the next slice has landed
+      pieces::lds_barrier();   // everywhere, and `now` has been read
+      __builtin_amdgcn_sched_barrier(0);
+      read(next, 0);
+      op.fetch(now, kt + 2);
+      oq.fetch(now + P::BYTES, kt + 2);
+      multiply(1);
+      interleave<P::MOVES + Q::MOVES>();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    pieces::wait_loads();      // nothing may still move into this workgroup's LDS
+  }
+
+  // spreads the LDS reads and fetches of half a slice between its products
+  template <int FETCHES>
+  __device__ __forceinline__ static void interleave() {
+    constexpr int PRODUCTS = IB * JB * (TYPE == OT_F32 ? 4 : 1);
+    constexpr int READS = (MP == KC ? IB : (TYPE == OT_F32 ? 4 : 2) * IB) + (MQ == KC ? JB : (TYPE == OT_F32 ? 4 : 2) * JB);
+    constexpr int PER = PRODUCTS / (READS + FETCHES) < 1 ? 1 : PRODUCTS / (READS + FETCHES);
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
+    for (int k = 0; k < READS; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);     // an LDS read
+      __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);   // products
+    }
 #pragma unroll
-        for (int j = 0; j < JB; ++j) fq[s][j] = Q::read(now + P::BYTES, wn * JB + j, s, lane);
-#pragma unroll
-        for (int i = 0; i < IB; ++i) fp[s][i] = P::read(now, wm * IB + i, s, lane);
-      }
-      if (kt + 1 < nk) {
-        op.fetch(next, kt + 1);
-        oq.fetch(next + P::BYTES, kt + 1);
-      }
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int i = 0; i < IB; ++i)
-#pragma unroll
-          for (int j = 0; j < JB; ++j) acc[i][j] = Mfma<TYPE>::mul(fq[s][j], fp[s][i], acc[i][j]);
+    for (int k = 0; k < FETCHES; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);     // a fetch
+      __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
     }
   }
 

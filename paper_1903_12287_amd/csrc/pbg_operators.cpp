@@ -215,7 +215,7 @@ extern "C" pbg_status pbg_group_linear_backward(pbg_ctx* ctx, int32_t dtype, con
     if (da) ops.add(&g.x, &g.ldx, n, in_dim);
     if (dx) ops.add(&g.a, &g.lda, gm, in_dim);
   }
-  if (da) plan_group_da(n, groups, out_dim, in_dim, &plan);
+  if (da) plan_group_da(dtype, n, groups, out_dim, in_dim, &plan);
   st = workspace(ctx, ops.bytes + (size_t)plan.partial_slots * out_dim * in_dim * 4);
   if (st != PBG_OK) return st;
   ops.place((char*)ctx->ops_ws);

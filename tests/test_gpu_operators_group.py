@@ -99,6 +99,14 @@ def test_few_rows_in_many_groups(ctx, t):
 
 
 @pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("sizes,k,m", [([2501, 0, 3100, 2700], 72, 2048), ([2501, 0, 3100, 2700], 2043, 61),
+                                       ([300, 513, 0, 290], 2048, 2048), ([257, 255, 900, 3], 1999, 2053)])
+def test_wide_products(ctx, t, sizes, k, m):
+    """Enough rows and columns for the largest tiles, forward, dx and da."""
+    run_case(ctx, TYPES[t], sizes, k, m, seed=1)
+
+
+@pytest.mark.parametrize("t", TYPES)
 def test_no_rows(ctx, t):
     dt = TYPES[t]
     a = torch.ones(3, 4, 5, dtype=dt, device="cuda")
