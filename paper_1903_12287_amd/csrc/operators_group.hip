@@ -15,34 +15,46 @@ using tile::KR;
 
 struct Launch {
   int shift;              // rows of a slot: 2^shift
-  int row_tiles, col_tiles;   // da: tiles of one matrix; else row_tiles is 1
+  int row_tiles, col_tiles;   // da: tiles of one matrix; y, dx: slots of all groups, tiles of the columns
   uint32_t blocks;
   bool vec;               // rows of the output start at multiples of four values
   float* partial;         // da: partial sums of the groups of several slots
 };
+
+// Tiles in bands of BAND slots, column by column: the workgroups that an XCD runs at a time share the rows of a few
+// slots and the matrix rows of a few columns, which its L2 then fetches once.
+template <int BAND>
+__device__ __forceinline__ void band_tile(uint32_t at, uint32_t slots, uint32_t cols, uint32_t& slot, uint32_t& col) {
+  const uint32_t band = at / (BAND * cols), r = at - band * (BAND * cols);
+  const uint32_t h = min((uint32_t)BAND, slots - BAND * band);
+  col = r / h;
+  slot = BAND * band + (r - col * h);
+}
 
 // y and dx: one slot of a group's rows, one tile of the output's columns
 template <int TYPE, int WHICH, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void group_rows_kernel(GroupArgs g, Launch L) {
   typedef tile::Tile<TYPE, KC, WHICH == GP_FORWARD ? KC : KR, BM, BN, WM, WN> Tl;
   constexpr int ES = TYPE == OT_F32 ? 4 : 2;
-  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  constexpr int BAND = BM >= 256 ? 4 : 8;
+  __shared__ __attribute__((aligned(1024))) char lds0[Tl::STAGE], lds1[Tl::STAGE];
   if (!args_good(g.bad, g.host_bad)) return;
   const uint32_t at = tile::xcd_place(blockIdx.x, L.blocks);
-  const int64_t slot = at / L.col_tiles;
-  const int j0 = (int)(at % L.col_tiles) * BN;
+  uint32_t slot, col;
+  band_tile<BAND>(at, L.row_tiles, L.col_tiles, slot, col);
+  const int j0 = (int)col * BN;
   const int grp = group_of_slot(g.offsets, g.groups, L.shift, slot);
   if (grp < 0) return;
-  const int64_t r0 = g.offsets[grp] + ((slot - first_slot(g.offsets, grp, L.shift)) << L.shift);
+  const int64_t r0 = g.offsets[grp] + (((int64_t)slot - first_slot(g.offsets, grp, L.shift)) << L.shift);
   const int rows = (int)min((int64_t)BM, g.offsets[grp + 1] - r0);
   if (rows <= 0) return;
   const char* a = (const char*)g.a + grp * g.a_group * ES;
   v4f acc[Tl::IB][Tl::JB];
   const int width = WHICH == GP_FORWARD ? g.m : g.k;
   if (WHICH == GP_FORWARD)
-    Tl::run(lds, (const char*)g.x + r0 * g.ldx * ES, g.ldx, rows, a + (int64_t)j0 * g.lda * ES, g.lda, g.m - j0, g.kd, acc);
+    Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.x + r0 * g.ldx * ES, g.ldx, rows, a + (int64_t)j0 * g.lda * ES, g.lda, g.m - j0, g.kd, acc);
   else
-    Tl::run(lds, (const char*)g.dy + r0 * g.lddy * ES, g.lddy, rows, a + (int64_t)j0 * ES, g.lda, g.kd - j0, g.m, acc);
+    Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.dy + r0 * g.lddy * ES, g.lddy, rows, a + (int64_t)j0 * ES, g.lda, g.kd - j0, g.m, acc);
   Tl::template store<TYPE>(acc, (char*)g.out + (r0 * g.ldo + j0) * ES, g.ldo, rows, width - j0, L.vec);
 }
 
@@ -57,7 +69,7 @@ template <int TYPE, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Launch L) {
   typedef tile::Tile<TYPE, KR, KR, BM, BN, WM, WN> Tl;
   constexpr int ES = TYPE == OT_F32 ? 4 : 2;
-  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  __shared__ __attribute__((aligned(1024))) char lds0[Tl::STAGE], lds1[Tl::STAGE];
   if (!args_good(g.bad, g.host_bad)) return;
   const uint32_t at = tile::xcd_place(blockIdx.x, L.blocks);
   const int tiles = L.row_tiles * L.col_tiles;
@@ -72,7 +84,7 @@ __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Lau
   if (part > 0 && r0 >= last) return;   // slot 0 of an empty group stores zeros
   const int64_t depth = min((int64_t)1 << L.shift, last - r0);
   v4f acc[Tl::IB][Tl::JB];
-  Tl::run(lds, (const char*)g.dy + (r0 * g.lddy + i0) * ES, g.lddy, g.md - i0, (const char*)g.x + (r0 * g.ldx + j0) * ES,
+  Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.dy + (r0 * g.lddy + i0) * ES, g.lddy, g.md - i0, (const char*)g.x + (r0 * g.ldx + j0) * ES,
           g.ldx, g.kd - j0, depth, acc);
   const int rows = min(BM, g.m - i0), cols = g.k - j0;
   if (last - first <= (int64_t)1 << L.shift) {
@@ -163,9 +175,10 @@ int64_t tiles_of(int64_t v, int b) { return (v + b - 1) / b; }
 template <int TYPE, int WHICH, int BM, int BN, int WM, int WN>
 bool launch_rows(const GroupArgs& g, Launch L, hipStream_t s) {
   L.shift = __builtin_ctz(BM);
-  L.row_tiles = 1;
+  const int64_t slots = (g.n >> L.shift) + g.groups;
+  L.row_tiles = (int)slots;
   L.col_tiles = (int)tiles_of(WHICH == GP_FORWARD ? g.m : g.k, BN);
-  const int64_t blocks = ((g.n >> L.shift) + g.groups) * L.col_tiles;
+  const int64_t blocks = slots * L.col_tiles;
   if (blocks * 64 * WM * WN >= 1ll << 32) return false;
   L.blocks = (uint32_t)blocks;
   group_rows_kernel<TYPE, WHICH, BM, BN, WM, WN><<<L.blocks, 64 * WM * WN, 0, s>>>(g, L);

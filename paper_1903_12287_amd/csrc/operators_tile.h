@@ -8,7 +8,8 @@
 // the buffer, which reads zero.  Rows start at multiples of 16 bytes and widths are multiples of 16 bytes: other
 // operands are copied into such a layout first (group_pack_kernel).
 //
-// LDS: two stages.  KC tiles are [x][128 bytes], the 16-byte group q of row x at q ^ (x & 7); KR tiles are
+// LDS: two stages, arrays of their own and named in the code (an LDS read behind a load to LDS otherwise waits for it,
+// wherever the two go).  KC tiles are [x][128 bytes], the 16-byte group q of row x at q ^ (x & 7); KR tiles are
 // [k][x], 16 bits: 32-byte pairs at p ^ f(k) (pieces::kr_f), read four rows at a time by the transposing LDS read;
 // 32 bits: 64-byte units at u ^ (k / 4), read a word a lane.  Either way the lanes of a read fall in distinct banks.
 #pragma once
@@ -19,6 +20,8 @@
 namespace tile {
 
 enum { KC = 0, KR = 1 };
+
+typedef __attribute__((address_space(3))) char lds_t;   // LDS by its own address space, so that an access names its array
 
 template <int TYPE> struct Mfma;
 template <> struct Mfma<OT_F32> {
@@ -93,36 +96,68 @@ struct Operand {
   }
 
   // slice kt into the stage at lds
-  __device__ __forceinline__ void fetch(char* lds, int kt) const {
+  __device__ __forceinline__ void fetch(lds_t* lds, int at, int kt) const {
     const rsrc_t rs = pieces::make_rsrc(base + kt * step);
 #pragma unroll
     for (int j = 0; j < MOVES; ++j) {
       const uint32_t o = (uint32_t)kt * KS + kat[j] < kdim ? off[j] : pieces::kOob;
-      pieces::dma16(rs, lds + (wave + NW * j) * 1024, o, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (pieces::lds_void*)(lds + (at + (wave + NW * j) * 1024)), 16, o, 0, 0, 0);
     }
   }
 
-  // the 16 rows from 16 blk on, summed indices of step s (half a slice)
-  __device__ __forceinline__ static typename Mfma<TYPE>::Frag read(const char* lds, int blk, int s, int lane) {
-    typedef typename Mfma<TYPE>::Frag Frag;
+  // Where this lane reads: places in the tile from which the constants of block and step lead on.  They are made
+  // opaque so that an address stays its array, a place and a constant: from longer chains the compiler loses which
+  // array it reads, and then waits for the loads to the other one too.
+  int place[2];
+  __device__ __forceinline__ void reader(int lane, int blk0) {
     const int l16 = lane & 15, g = lane >> 4;
-    if constexpr (MODE == KC) {
-      return *(const Frag*)(lds + (16 * blk + l16) * 128 + (((4 * s + g) ^ (l16 & 7)) << 4));
-    } else if constexpr (TYPE == OT_F32) {
-      Frag f;
-      const char* p = lds + (16 * s + 4 * g) * (BX * 4) + ((blk ^ (g & UM)) << 6) + l16 * 4;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) f[j] = *(const float*)(p + j * BX * 4);
-      return f;
+    if (MODE == KC) {
+      place[0] = (16 * blk0 + l16) * 128 + ((g ^ (l16 & 7)) << 4);
+      place[1] = (16 * blk0 + l16) * 128 + (((4 + g) ^ (l16 & 7)) << 4);
+    } else if (TYPE == OT_F32) {
+      place[0] = 4 * g * (BX * 4) + (((g & UM) ^ blk0) << 6) + l16 * 4;
+      place[1] = 0;
     } else {
       const int row = 8 * g + (l16 >> 2);
-      const uint32_t at = pieces::lds_offset(lds) + s * 32 * (BX * 2);
-      const uint32_t a0 = (uint32_t)(row * BX * 2 + ((kr_swizzle(row) ^ blk) << 5) + (l16 & 3) * 8);
-      const uint32_t a1 = (uint32_t)((row + 4) * BX * 2 + ((kr_swizzle(row + 4) ^ blk) << 5) + (l16 & 3) * 8);
-      return __builtin_bit_cast(Frag, pieces::kr_fragment(at + a0, at + a1));
+      place[0] = row * BX * 2 + ((kr_swizzle(row) ^ blk0) << 5) + (l16 & 3) * 8;
+      place[1] = (row + 4) * BX * 2 + ((kr_swizzle(row + 4) ^ blk0) << 5) + (l16 & 3) * 8;
+    }
+    __asm__("" : "+v"(place[0]), "+v"(place[1]));
+  }
+
+  // the wave's 16 rows from 16 blk on, summed indices of step s (half a slice), of the operand `at` bytes into the stage
+  __device__ __forceinline__ typename Mfma<TYPE>::Frag read(const lds_t* lds, int at, int blk, int s) const {
+    typedef typename Mfma<TYPE>::Frag Frag;
+    if constexpr (MODE == KC) {
+      return *(const __attribute__((address_space(3))) Frag*)(lds + place[s] + (at + blk * 2048));
+    } else if constexpr (TYPE == OT_F32) {
+      Frag f;
+      const int o = place[0] ^ (blk << 6);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        f[j] = *(const __attribute__((address_space(3))) float*)(lds + o + (at + (16 * s + j) * BX * 4));
+      return f;
+    } else {
+      const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((pieces::lds_v4s*)(lds + (place[0] ^ (blk << 5)) + (at + s * 64 * BX)));
+      const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((pieces::lds_v4s*)(lds + (place[1] ^ (blk << 5)) + (at + s * 64 * BX)));
+      typedef short v8s __attribute__((ext_vector_type(8)));
+      return __builtin_bit_cast(Frag, (v8s)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   }
 };
+
+// A workgroup barrier behind this wave's LDS reads and all but the last N of its loads to LDS.  (A fence for LDS
+// contents in its place waits for every load to LDS: the next slice's too.)
+template <int N>
+__device__ __forceinline__ void stage_barrier() {
+  static_assert(N < 64, "six bits");
+  __builtin_amdgcn_sched_barrier(0);
+  __asm__ volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | ((N >> 4) << 14));   // vmcnt(N) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  __asm__ volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 // A BM x BN tile by WM x WN waves, each (BM / WM) x (BN / WN) of it.
 template <int TYPE, int MP, int MQ, int BM, int BN, int WM, int WN>
@@ -132,80 +167,101 @@ struct Tile {
   typedef Operand<TYPE, MP, BM, NW> P;
   typedef Operand<TYPE, MQ, BN, NW> Q;
   static constexpr int STAGE = P::BYTES + Q::BYTES;
-  static constexpr int LDS = 2 * STAGE;
   static constexpr int KS = P::KS;
+  static constexpr int FETCHES = P::MOVES + Q::MOVES;
+  static constexpr int READS = (MP == KC ? IB : (TYPE == OT_F32 ? 4 : 2) * IB) + (MQ == KC ? JB : (TYPE == OT_F32 ? 4 : 2) * JB);
 
   // acc[i][j][r]: row 16 i + lane % 16, column 16 j + 4 (lane / 16) + r of the wave's part (Q feeds the matrix
   // instruction's rows, so that a lane holds four consecutive columns of C)
-  __device__ __forceinline__ static void run(char* lds, const void* p, int64_t ldp, int rows, const void* q, int64_t ldq,
+  __device__ __forceinline__ static void run(lds_t* lds0, lds_t* lds1, const void* p, int64_t ldp, int rows, const void* q, int64_t ldq,
                                              int cols, int64_t depth, v4f (&acc)[IB][JB]) {
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = w / WN, wn = w % WN;
     P op;
     Q oq;
     op.open(p, ldp, rows, depth, w, lane);
+    op.reader(lane, wm * IB);
     oq.open(q, ldq, cols, depth, w, lane);
+    oq.reader(lane, wn * JB);
 #pragma unroll
     for (int i = 0; i < IB; ++i)
 #pragma unroll
       for (int j = 0; j < JB; ++j) acc[i][j] = (v4f){0.f, 0.f, 0.f, 0.f};
-    const int nk = (int)((depth + KS - 1) / KS);
+    const int nk = (int)((depth + 2 * KS - 1) / (2 * KS)) * 2;   // an even number of slices
     if (nk == 0) return;
-    op.fetch(lds, 0);
-    oq.fetch(lds + P::BYTES, 0);
-    typename Mfma<TYPE>::Frag fp[2][IB], fq[2][JB];
-    auto read = [&](const char* stage, int s) {
-#pragma unroll
-      for (int j = 0; j < JB; ++j) fq[s][j] = Q::read(stage + P::BYTES, wn * JB + j, s, lane);
-#pragma unroll
-      for (int i = 0; i < IB; ++i) fp[s][i] = P::read(stage, wm * IB + i, s, lane);
+    auto fetch = [&](lds_t* stage, int kt) {
+      op.fetch(stage, 0, kt);
+      oq.fetch(stage, P::BYTES, kt);
     };
-    auto multiply = [&](int s) {
+    fetch(lds0, 0);
+    fetch(lds1, 1);
+    stage_barrier<FETCHES>();    // slice 0 has landed
+    if (wm * IB * 16 >= rows || wn * JB * 16 >= cols) {
+      // nothing of this wave's part is stored: it only moves its share, and leaves the matrix unit to the others
+      for (int kt = 0; kt < nk; kt += 2) {
+        stage_barrier<FETCHES>();
+        fetch(lds0, kt + 2);
+        stage_barrier<FETCHES>();
+        stage_barrier<FETCHES>();
+        fetch(lds1, kt + 3);
+        stage_barrier<FETCHES>();
+      }
+      pieces::wait_loads();
+      return;
+    }
+    typename Mfma<TYPE>::Frag fp[2][IB], fq[2][JB];
+    auto read = [&](const lds_t* stage, int s) {
 #pragma unroll
-      for (int i = 0; i < IB; ++i)
+      for (int j = 0; j < JB; ++j) fq[s][j] = oq.read(stage, P::BYTES, j, s);
+#pragma unroll
+      for (int i = 0; i < IB; ++i) fp[s][i] = op.read(stage, 0, i, s);
+    };
+    auto multiply = [&](int s, int i0, int i1) {
+#pragma unroll
+      for (int i = i0; i < i1; ++i)
 #pragma unroll
         for (int j = 0; j < JB; ++j) acc[i][j] = Mfma<TYPE>::mul(fq[s][j], fp[s][i], acc[i][j]);
     };
-    pieces::wait_loads();      // this wave's part of the slice has landed,
-    pieces::lds_barrier();     // and everyone's
-    read(lds, 0);
-    op.fetch(lds + STAGE, 1);
-    oq.fetch(lds + STAGE + P::BYTES, 1);
-    // Half a slice is multiplied while the next half is read and the slice behind it fetched: one barrier a slice.
-    // The last two rounds fetch past the operands, which moves zeros, so that a round is one block of code.
-    for (int kt = 0; kt < nk; ++kt) {
-      char* now = lds + (kt & 1) * STAGE;
-      char* next = lds + (~kt & 1) * STAGE;
+    // A slice's first half is multiplied while its second is read; then everyone has read the stage, and the slice
+    // two further on is fetched into it, which has a slice and a half to arrive; the second half is multiplied while
+    // the next slice's first is read.  (With one barrier, fetches issued behind the first half: 0.7 slices to arrive,
+    // and 41 % of the waves' time spent waiting.)  The last rounds fetch and read past the operands, zeros, so that a
+    // round is one block of code.
+    constexpr int IH = (IB + 1) / 2;
+    auto round = [&](lds_t* now, const lds_t* next, int kt) {
       read(now, 1);
-      multiply(0);
-      interleave<0>();
-      __builtin_amdgcn_sched_barrier(0);   // the products stay ahead of the wait
-      pieces::wait_loads();    // the next slice has landed
-      pieces::lds_barrier();   // everywhere, and `now` has been read
-      __builtin_amdgcn_sched_barrier(0);
+      multiply(0, 0, IH);
+      interleave<READS, 0, IH * JB>();
+      stage_barrier<FETCHES>();    // everyone has read the stage
+      fetch(now, kt + 2);
+      multiply(0, IH, IB);
+      interleave<0, FETCHES, (IB - IH) * JB>();
+      stage_barrier<FETCHES>();    // slice kt + 1 has landed
       read(next, 0);
-      op.fetch(now, kt + 2);
-      oq.fetch(now + P::BYTES, kt + 2);
-      multiply(1);
-      interleave<P::MOVES + Q::MOVES>();
+      multiply(1, 0, IB);
+      interleave<READS, 0, IB * JB>();
       __builtin_amdgcn_sched_barrier(0);
+    };
+    read(lds0, 0);
+    for (int kt = 0; kt < nk; kt += 2) {
+      round(lds0, lds1, kt);
+      round(lds1, lds0, kt + 1);
     }
     pieces::wait_loads();      // nothing may still move into this workgroup's LDS
   }
 
-  // spreads the LDS reads and fetches of half a slice between its products
-  template <int FETCHES>
+  // spreads LDS reads and fetches between the products of a part of a round
+  template <int NR, int NF, int BLOCKS>
   __device__ __forceinline__ static void interleave() {
-    constexpr int PRODUCTS = IB * JB * (TYPE == OT_F32 ? 4 : 1);
-    constexpr int READS = (MP == KC ? IB : (TYPE == OT_F32 ? 4 : 2) * IB) + (MQ == KC ? JB : (TYPE == OT_F32 ? 4 : 2) * JB);
-    constexpr int PER = PRODUCTS / (READS + FETCHES) < 1 ? 1 : PRODUCTS / (READS + FETCHES);
+    constexpr int PRODUCTS = BLOCKS * (TYPE == OT_F32 ? 4 : 1);
+    constexpr int PER = PRODUCTS / (NR + NF) < 1 ? 1 : PRODUCTS / (NR + NF);
 #pragma unroll
-    for (int k = 0; k < READS; ++k) {
+    for (int k = 0; k < NR; ++k) {
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);     // an LDS read
       __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);   // products
     }
 #pragma unroll
-    for (int k = 0; k < FETCHES; ++k) {
+    for (int k = 0; k < NF; ++k) {
       __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);     // a fetch
       __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
     }
