@@ -35,13 +35,12 @@ struct GroupArgs {
 };
 
 struct GroupPlan {
-  bool da_wide;            // da: tiles of 256 x 256
   int da_shift;            // da: rows of a slot, 2^da_shift
   int64_t partial_slots;   // slots of partial sums, m k floats each (0: no group is longer than a slot)
   float* partial;
 };
 
-void plan_group_da(int type, int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p);
+void plan_group_da(int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p);
 // up to three operands into rows of wp values, a multiple of 16 bytes, zeros behind `width`
 void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,
                        const int64_t* rows, const int* width, const int* wp, hipStream_t s);
@@ -63,20 +62,24 @@ struct PrefArgs {
   float* logp;
   float* dlogp;          // written by the loss, read by its backward
   float* stats;          // [n][2]
-  double* picked;        // workspace: each row's log probability (0 where it does not count)
+  double* picked;        // workspace: each row's log probability (0 where it does not count), or
+  float2* parts;         // the stats of its segments, `splits` a row (0: rows are not cut)
+  int splits;
   void* dlogits;
   int64_t lddl;
   uint32_t* bad;
   uint32_t* host_bad;
 };
 
-void launch_check_labels(const PrefArgs& p, hipStream_t s);
+// segments of a row where they are few, else 0
+int preference_splits(int64_t n, int V);
+// the checks of labels and offsets, then the work
 void launch_preference_loss(const PrefArgs& p, int type, hipStream_t s);
 void launch_preference_backward(const PrefArgs& p, int type, hipStream_t s);
 
 // ---- clipping -----------------------------------------------------------------------------------
 constexpr int kClipBatch = 96;          // tensors a launch takes (its arguments hold their descriptors)
-constexpr int kClipBlock = 16384;       // values a workgroup takes
+constexpr int kClipBlock = 8192;        // values a workgroup takes
 
 struct ClipBatch {
   const void* g[kClipBatch];
@@ -87,8 +90,6 @@ struct ClipBatch {
   int32_t n;
 };
 
-// the sums of squares of the batch's blocks into parts
-void launch_clip_squares(const ClipBatch& b, double* parts, hipStream_t s);
-// norm and factor from all parts: scale[0] = the factor; *host_norm = the norm
-void launch_clip_factor(const double* parts, int64_t n, double max_norm, double* scale, double* host_norm, hipStream_t s);
-void launch_clip_scale(const ClipBatch& b, const double* scale, hipStream_t s);
+// all batches: sums of squares into parts (one a workgroup, `blocks` in all), the norm into *host_norm, the scaling
+void launch_clip(const ClipBatch* b, int batches, int64_t blocks, double max_norm, double* scale, double* parts,
+                 double* host_norm, hipStream_t s);

@@ -9,6 +9,21 @@ template <> struct Elem<OT_F32> { typedef float T; };
 template <> struct Elem<OT_BF16> { typedef __bf16 T; };
 template <> struct Elem<OT_F16> { typedef _Float16 T; };
 
+// 16 bytes of values at any place that their type allows (the hardware reads and writes them so)
+template <int TYPE> struct Vec;
+template <> struct Vec<OT_F32> {
+  static constexpr int N = 4;
+  typedef float V __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <> struct Vec<OT_BF16> {
+  static constexpr int N = 8;
+  typedef __bf16 V __attribute__((ext_vector_type(8), aligned(2)));
+};
+template <> struct Vec<OT_F16> {
+  static constexpr int N = 8;
+  typedef _Float16 V __attribute__((ext_vector_type(8), aligned(2)));
+};
+
 // A workgroup's verdict on the call's arguments: true where the checks ahead of it found nothing.  The first
 // workgroup hands the word to the host otherwise.
 __device__ __forceinline__ bool args_good(const uint32_t* bad, uint32_t* host_bad) {

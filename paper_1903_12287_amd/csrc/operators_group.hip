@@ -215,11 +215,7 @@ bool launch_typed(const GroupArgs& g, int which, const GroupPlan& p, hipStream_t
   if (which == GP_DA) {
     L.shift = p.da_shift;
     L.partial = p.partial;
-    if constexpr (TYPE != OT_F32) {
-      if (p.da_wide ? !launch_da<TYPE, 256, 256, 2, 4>(g, L, s) : !launch_da<TYPE, 128, 128, 2, 2>(g, L, s)) return false;
-    } else {
-      if (!launch_da<TYPE, 128, 128, 2, 2>(g, L, s)) return false;
-    }
+    if (!launch_da<TYPE, 128, 128, 2, 2>(g, L, s)) return false;
     if (p.partial_slots > 0) {
       const int64_t mk = (int64_t)g.m * g.k;
       const dim3 grid((unsigned)std::min<int64_t>(tiles_of(mk, 64), 4096), (unsigned)p.partial_slots);
@@ -248,12 +244,10 @@ void launch_check_offsets(const int64_t* offsets, int groups, int64_t n, uint32_
   check_offsets_kernel<<<blocks < 1024 ? blocks : 1024, 256, 0, s>>>(offsets, groups, n, flag);
 }
 
-void plan_group_da(int type, int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p) {
+void plan_group_da(int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p) {
   // Rows of a slot: enough slots for a few workgroups on each of the 256 compute units, where the matrices' tiles
   // alone are not; with tiles enough, only groups of four times the average and more are cut.
-  p->da_wide = type != OT_F32 && groups * tiles_of(m, 256) * tiles_of(k, 256) >= 256 && n / groups >= 2048;
-  const int b = p->da_wide ? 256 : 128;
-  const int64_t tiles = tiles_of(m, b) * tiles_of(k, b);
+  const int64_t tiles = tiles_of(m, 128) * tiles_of(k, 128);
   int64_t rows = std::max<int64_t>(256, n * tiles / 1024);
   if (groups * tiles >= 512) rows = std::max(rows, 4 * n / groups);
   int shift = 8;

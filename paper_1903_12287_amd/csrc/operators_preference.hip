@@ -2,32 +2,113 @@
 //
 // A row's log probability is l = z[y] - m - log sum_v exp(z[v] - m) with its largest score m: one pass over the row
 // keeps the running maximum and the sum relative to it.  The gradient of the row is
-// dlogp (1[v = y] - exp(z[v] - m - log sum)), a second pass over the scores once the pairs' losses are known.
+// dlogp (1[v = y] - exp(z[v] - m - log sum)), a second pass over the scores once the pairs' losses are known (a pair's
+// loss needs every row of both sequences).  m and log sum are kept apart, so that z - m stays exact however far from
+// zero the scores lie.
+//
+// Bound by memory: the scores are read for the loss, read again and overwritten by the gradient.  Rows without a label
+// are not read.  16 bytes a load wherever the row starts; a wave takes a row of up to 2,048 candidates, a workgroup a
+// longer one, and few rows are cut into segments whose (m, sum) are joined afterwards.
+#include <algorithm>
+
 #include "operators_device.h"
 
 namespace {
 
-// (m, s) of the union of two sets of scores, s relative to m; an empty set is (-inf, 0)
-__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
-  const float top = fmaxf(m, m2);
-  if (top == -INFINITY) {
-    s += s2;   // both empty, or a NaN
-    return;
-  }
-  s = s * expf(m - top) + s2 * expf(m2 - top);
-  m = top;
+// exp(d): base 2 through the hardware, whose argument d log2(e) is rounded; float32 scores get the rest back (their
+// gradient keeps more than 16 bits)
+template <int TYPE>
+__device__ __forceinline__ float exp_of(float d) {
+  constexpr float L = 1.44269502f, LL = 1.92596299e-8f;   // log2(e) in two parts
+  const float t = d * L;
+  const float r = __builtin_amdgcn_exp2f(t);
+  if (TYPE != OT_F32) return r;
+  // what t leaves out; 0 where it is not a number (infinite d) or r has vanished
+  const float e = fmaf(d, L, -t) + d * LL;
+  return r > 0.0f && r < INFINITY ? fmaf(r, e * 0.693147181f, r) : r;
 }
 
+// the largest score and the sum relative to it, of a set of scores; an empty set is (-inf, 0)
+struct Stats {
+  float m, s;
+};
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
+
 template <int TYPE>
+__device__ __forceinline__ void join(Stats& a, const Stats& b) {
+  const float m = fmaxf(a.m, b.m), base = base_of(m);
+  a.s = a.s * exp_of<TYPE>(a.m - base) + b.s * exp_of<TYPE>(b.m - base);
+  a.m = m;
+}
+
+// values [first, last) of a row by THREADS threads, U loads of 16 bytes on their way at a time
+template <int TYPE, int THREADS>
+__device__ __forceinline__ Stats scan(const typename Elem<TYPE>::T* z, int first, int last, int tid) {
+  typedef typename Vec<TYPE>::V V;
+  constexpr int N = Vec<TYPE>::N, U = 4;
+  Stats a = {-INFINITY, 0.0f};
+  for (int v0 = first; v0 < last; v0 += THREADS * N * U) {
+    float x[U * N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int v = v0 + (u * THREADS + tid) * N;
+      if (v + N <= last) {
+        const V w = *(const V*)(z + v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[u * N + j] = (float)w[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[u * N + j] = v + j < last ? (float)z[v + j] : -INFINITY;
+      }
+    }
+    float m = a.m;
+#pragma unroll
+    for (int i = 0; i < U * N; ++i) m = fmaxf(m, x[i]);
+    const float base = base_of(m);
+    float s[4] = {a.s * exp_of<TYPE>(a.m - base), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < U * N; ++i) s[i & 3] += exp_of<TYPE>(x[i] - base);
+    a.m = m;
+    a.s = (s[0] + s[1]) + (s[2] + s[3]);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const Stats b = {__shfl_xor(a.m, o, 64), __shfl_xor(a.s, o, 64)};
+    join<TYPE>(a, b);
+  }
+  return a;
+}
+
+// a workgroup's stats from its waves', in thread 0
+template <int TYPE>
+__device__ __forceinline__ Stats join_waves(Stats a) {
+  __shared__ Stats part[4];
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = a;
+  __syncthreads();
+  a = part[0];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) join<TYPE>(a, part[w]);
+  return a;
+}
+
+// a counted row's stats and log probability; a row without a distribution does not count
+__device__ __forceinline__ void finish_row(const Stats& a, float z_label, float2& stats, double& picked) {
+  const bool none = a.m == -INFINITY && a.s == 0.0f;
+  const float ls = none ? 0.0f : logf(a.s);
+  stats = make_float2(a.m, ls);
+  picked = none ? 0.0 : (double)(z_label - a.m) - (double)ls;
+}
+
+// Many rows, whose labels and offsets have been checked: WAVE, a wave a row, else a workgroup.
+template <int TYPE, bool WAVE>
 __global__ __launch_bounds__(256) void row_stats_kernel(PrefArgs p) {
   typedef typename Elem<TYPE>::T T;
-  __shared__ float sm[4], ss[4];
   if (!args_good(p.bad, p.host_bad)) return;
-  const int64_t t = blockIdx.x;
-  const int tid = threadIdx.x;
-  if (t >= p.n) return;   // no rows: the launch only hands over the verdict
-  if (sequence_of_row(p.offsets, 2 * p.pairs, t) < 0) return;
+  const int64_t t = WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  const int tid = WAVE ? threadIdx.x & 63 : threadIdx.x;
+  if (t >= p.n) return;
   const int label = p.labels[t];
+  if (sequence_of_row(p.offsets, 2 * p.pairs, t) < 0) return;
   if (label < 0) {
     if (tid == 0) {
       p.stats[2 * t] = p.stats[2 * t + 1] = 0.0f;
@@ -36,39 +117,74 @@ __global__ __launch_bounds__(256) void row_stats_kernel(PrefArgs p) {
     return;
   }
   const T* z = (const T*)p.logits + t * p.ld;
-  float m = -INFINITY, s = 0.0f;
-  for (int v = tid; v < p.V; v += 256) {
-    const float x = (float)z[v];
-    join(m, s, x, x == -INFINITY ? 0.0f : (x == x ? 1.0f : x));
-  }
-  for (int o = 32; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(s, o, 64);
-    join(m, s, m2, s2);
-  }
-  if ((tid & 63) == 0) {
-    sm[tid >> 6] = m;
-    ss[tid >> 6] = s;
-  }
-  __syncthreads();
+  const float z_label = (float)z[label];
+  Stats a;
+  if (WAVE) a = scan<TYPE, 64>(z, 0, p.V, tid);
+  else a = join_waves<TYPE>(scan<TYPE, 256>(z, 0, p.V, tid));
   if (tid) return;
-  for (int w = 1; w < 4; ++w) join(m, s, sm[w], ss[w]);
-  const bool none = m == -INFINITY && s == 0.0f;
-  const float ls = none ? 0.0f : logf(s);
-  p.stats[2 * t] = m;
-  p.stats[2 * t + 1] = ls;
-  p.picked[t] = none ? 0.0 : (double)((float)z[label] - m) - (double)ls;
+  float2 st;
+  finish_row(a, z_label, st, p.picked[t]);
+  p.stats[2 * t] = st.x;
+  p.stats[2 * t + 1] = st.y;
 }
 
-// one workgroup per pair: each sequence's rows are added in a fixed order
-__global__ __launch_bounds__(256) void pair_loss_kernel(PrefArgs p) {
-  __shared__ double part[2][4];
+// Few rows: segment blockIdx.x % splits of row blockIdx.x / splits, and the checks of the call's labels and offsets on
+// the way.  Nothing but the workspace is written.
+template <int TYPE>
+__global__ __launch_bounds__(256) void row_parts_kernel(PrefArgs p) {
+  typedef typename Elem<TYPE>::T T;
+  const int64_t t = blockIdx.x / p.splits;
+  const int part = blockIdx.x % p.splits, tid = threadIdx.x;
+  const int sequences = 2 * p.pairs;
+  if (blockIdx.x == 0) {
+    bool bad = false;
+    for (int i = tid; i <= sequences; i += 256) {
+      const int64_t v = p.offsets[i];
+      bad |= v < 0 || v > p.n || (i < sequences && p.offsets[i + 1] < v);
+    }
+    if (__ballot(bad) && (tid & 63) == 0) atomicOr(p.bad, (uint32_t)OPS_BAD_OFFSETS);
+  }
+  if (t >= p.n) return;
+  const int label = p.labels[t];
+  if (t < p.offsets[0] || t >= p.offsets[sequences]) return;
+  if (label >= p.V && tid == 0) atomicOr(p.bad, (uint32_t)OPS_BAD_LABEL);
+  if (label < 0 || label >= p.V) return;
+  const int per = ((p.V + p.splits - 1) / p.splits + 255) & ~255;
+  const int first = min(p.V, part * per), last = min(p.V, first + per);
+  const Stats a = join_waves<TYPE>(scan<TYPE, 256>((const T*)p.logits + t * p.ld, first, last, tid));
+  if (tid == 0) ((Stats*)p.parts)[blockIdx.x] = a;
+}
+
+// One workgroup per pair: each sequence's rows are added in a fixed order.  FEW: their segments are joined first.
+template <int TYPE, bool FEW>
+__global__ __launch_bounds__(1024) void pair_loss_kernel(PrefArgs p) {
+  typedef typename Elem<TYPE>::T T;
+  __shared__ double part[2][16];
   if (!args_good(p.bad, p.host_bad)) return;
   const int64_t pair = blockIdx.x;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, waves = blockDim.x >> 6;
   for (int w = 0; w < 2; ++w) {
     double s = 0.0;
     const int64_t end = p.offsets[2 * pair + w + 1];
-    for (int64_t t = p.offsets[2 * pair + w] + tid; t < end; t += 256) s += p.picked[t];
+    for (int64_t t = p.offsets[2 * pair + w] + tid; t < end; t += blockDim.x) {
+      if (FEW) {
+        const int label = p.labels[t];
+        float2 st = make_float2(0.0f, 0.0f);
+        double l = 0.0;
+        if (label >= 0) {
+          const Stats* q = (const Stats*)p.parts + t * p.splits;
+          const float z_label = (float)((const T*)p.logits)[t * p.ld + label];
+          Stats a = q[0];
+          for (int i = 1; i < p.splits; ++i) join<TYPE>(a, q[i]);
+          finish_row(a, z_label, st, l);
+        }
+        p.stats[2 * t] = st.x;
+        p.stats[2 * t + 1] = st.y;
+        s += l;
+      } else {
+        s += p.picked[t];
+      }
+    }
     s = wave_sum_d(s);
     if ((tid & 63) == 0) part[w][tid >> 6] = s;
   }
@@ -76,7 +192,8 @@ __global__ __launch_bounds__(256) void pair_loss_kernel(PrefArgs p) {
   if (tid) return;
   double lp[2], ratio[2];
   for (int w = 0; w < 2; ++w) {
-    lp[w] = part[w][0] + part[w][1] + part[w][2] + part[w][3];
+    lp[w] = part[w][0];
+    for (int i = 1; i < waves; ++i) lp[w] += part[w][i];
     ratio[w] = lp[w] - (p.ref ? (double)p.ref[2 * pair + w] : 0.0);
     p.logp[2 * pair + w] = (float)lp[w];
   }
@@ -94,54 +211,139 @@ __global__ __launch_bounds__(256) void pair_loss_kernel(PrefArgs p) {
   }
 }
 
-template <int TYPE>
-__global__ __launch_bounds__(256) void preference_backward_kernel(PrefArgs p) {
+// segment `part` of `splits` of a row's gradient
+template <int TYPE, int THREADS>
+__device__ __forceinline__ void row_gradient(const PrefArgs& p, int64_t t, int part, int tid) {
   typedef typename Elem<TYPE>::T T;
-  if (!args_good(p.bad, p.host_bad)) return;
-  const int64_t t = blockIdx.x;
-  if (t >= p.n) return;
+  typedef typename Vec<TYPE>::V V;
+  constexpr int N = Vec<TYPE>::N, U = 4;
+  const int label = p.labels[t];
   const int q = sequence_of_row(p.offsets, 2 * p.pairs, t);
   if (q < 0) return;
-  const int label = p.labels[t];
   const T* z = (const T*)p.logits + t * p.ld;
   T* dz = (T*)p.dlogits + t * p.lddl;
   const float m = p.stats[2 * t], ls = p.stats[2 * t + 1];
   const bool counts = label >= 0 && !(m == -INFINITY && ls == 0.0f);
   const float g = p.dlogp[q];
-  for (int v = threadIdx.x; v < p.V; v += 256) {
-    float d = 0.0f;
-    if (counts) d = g * ((v == label ? 1.0f : 0.0f) - expf((float)z[v] - m - ls));
-    dz[v] = (T)d;
+  const int per = ((p.V + p.splits - 1) / p.splits + 255) & ~255;
+  const int first = min(p.V, part * per), last = min(p.V, first + per);
+  if (!counts) {
+    for (int v = first + tid * N; v < last; v += THREADS * N) {
+      if (v + N <= last) {
+        V w;
+#pragma unroll
+        for (int j = 0; j < N; ++j) w[j] = (T)0.0f;
+        *(V*)(dz + v) = w;
+      } else {
+        for (int j = v; j < last; ++j) dz[j] = (T)0.0f;
+      }
+    }
+    return;
+  }
+  auto slope = [&](float x, int v) {
+    const float pr = exp_of<TYPE>((x - m) - ls);
+    return (T)(g * ((v == label ? 1.0f : 0.0f) - pr));
+  };
+  for (int v0 = first; v0 < last; v0 += THREADS * N * U) {
+    V w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int v = v0 + (u * THREADS + tid) * N;
+      if (v + N <= last) w[u] = *(const V*)(z + v);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int v = v0 + (u * THREADS + tid) * N;
+      if (v + N <= last) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) w[u][j] = slope((float)w[u][j], v + j);
+        *(V*)(dz + v) = w[u];
+      } else {
+        for (int j = v; j < last; ++j) dz[j] = slope((float)z[j], j);
+      }
+    }
   }
 }
 
-// labels of rows inside a sequence are below V (negative ones do not count)
-__global__ __launch_bounds__(256) void check_labels_kernel(PrefArgs p) {
-  const int64_t first = p.offsets[0], last = p.offsets[2 * p.pairs];
-  bool bad = false;
-  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < p.n; t += (int64_t)gridDim.x * 256)
-    bad |= t >= first && t < last && p.labels[t] >= p.V;
-  if (__ballot(bad) && (threadIdx.x & 63) == 0) atomicOr(p.bad, (uint32_t)OPS_BAD_LABEL);
+template <int TYPE, bool WAVE>
+__global__ __launch_bounds__(256) void preference_backward_kernel(PrefArgs p) {
+  if (!args_good(p.bad, p.host_bad)) return;
+  if (WAVE) {
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t < p.n) row_gradient<TYPE, 64>(p, t, 0, threadIdx.x & 63);
+  } else {
+    const int64_t t = blockIdx.x / p.splits;
+    if (t < p.n) row_gradient<TYPE, 256>(p, t, blockIdx.x % p.splits, threadIdx.x);
+  }
+}
+
+// offsets nondecreasing within [0, n]; labels of rows inside a sequence below V (negative ones do not count)
+__global__ __launch_bounds__(256) void check_preference_kernel(PrefArgs p) {
+  const int sequences = 2 * p.pairs;
+  const int64_t first = p.offsets[0], last = p.offsets[sequences];
+  const int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+  uint32_t bad = 0;
+  for (int64_t i = i0; i <= sequences; i += step) {
+    const int64_t v = p.offsets[i];
+    if (v < 0 || v > p.n || (i < sequences && p.offsets[i + 1] < v)) bad |= OPS_BAD_OFFSETS;
+  }
+  for (int64_t t = i0; t < p.n; t += step)
+    if (t >= first && t < last && p.labels[t] >= p.V) bad |= OPS_BAD_LABEL;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) bad |= (uint32_t)__shfl_xor((int)bad, o, 64);
+  if (bad && (threadIdx.x & 63) == 0) atomicOr(p.bad, bad);
+}
+
+void check(const PrefArgs& p, hipStream_t s) {
+  const int64_t work = std::max<int64_t>(p.n, 2 * (int64_t)p.pairs + 1);
+  check_preference_kernel<<<(unsigned)std::min<int64_t>((work + 255) / 256, 1024), 256, 0, s>>>(p);
+}
+
+// a wave takes a row of up to so many candidates: 32 loads a lane at most
+constexpr int kWaveRow = 2048;
+
+template <int TYPE>
+void launch_loss_typed(const PrefArgs& p, hipStream_t s) {
+  if (p.splits > 0) {
+    row_parts_kernel<TYPE><<<(unsigned)(std::max<int64_t>(p.n, 1) * p.splits), 256, 0, s>>>(p);
+    pair_loss_kernel<TYPE, true><<<p.pairs, 256, 0, s>>>(p);
+    return;
+  }
+  check(p, s);
+  if (p.V <= kWaveRow) row_stats_kernel<TYPE, true><<<(unsigned)((p.n + 3) / 4), 256, 0, s>>>(p);
+  else row_stats_kernel<TYPE, false><<<(unsigned)p.n, 256, 0, s>>>(p);
+  pair_loss_kernel<TYPE, false><<<p.pairs, p.n / p.pairs > 8192 ? 1024 : 256, 0, s>>>(p);
+}
+
+template <int TYPE>
+void launch_backward_typed(PrefArgs p, hipStream_t s) {
+  check(p, s);
+  if (p.V <= kWaveRow) {
+    preference_backward_kernel<TYPE, true><<<(unsigned)((std::max<int64_t>(p.n, 1) + 3) / 4), 256, 0, s>>>(p);
+  } else {
+    // four workgroups and more on each of the 256 compute units where there are few rows
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.V / 2048, 2048 / std::max<int64_t>(p.n, 1)));
+    preference_backward_kernel<TYPE, false><<<(unsigned)(std::max<int64_t>(p.n, 1) * p.splits), 256, 0, s>>>(p);
+  }
 }
 
 }  // namespace
 
-void launch_check_labels(const PrefArgs& p, hipStream_t s) {
-  const int64_t blocks = (p.n + 255) / 256;
-  check_labels_kernel<<<(unsigned)(blocks < 1 ? 1 : (blocks > 1024 ? 1024 : blocks)), 256, 0, s>>>(p);
+int preference_splits(int64_t n, int V) {
+  // Few rows: their stats are finished by the pairs' workgroups, a thread a row, which saves a launch and lets long
+  // rows be cut.  Up to 2,048 rows; segments of 4,096 candidates and more, as many as give the chip work.
+  if (n > 2048) return 0;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(V / 4096, 2048 / std::max<int64_t>(n, 1)));
 }
 
 void launch_preference_loss(const PrefArgs& p, int type, hipStream_t s) {
-  const unsigned rows = p.n > 0 ? (unsigned)p.n : 1u;
-  if (type == OT_F32) row_stats_kernel<OT_F32><<<rows, 256, 0, s>>>(p);
-  else if (type == OT_BF16) row_stats_kernel<OT_BF16><<<rows, 256, 0, s>>>(p);
-  else row_stats_kernel<OT_F16><<<rows, 256, 0, s>>>(p);
-  pair_loss_kernel<<<p.pairs, 256, 0, s>>>(p);
+  if (type == OT_F32) launch_loss_typed<OT_F32>(p, s);
+  else if (type == OT_BF16) launch_loss_typed<OT_BF16>(p, s);
+  else launch_loss_typed<OT_F16>(p, s);
 }
 
 void launch_preference_backward(const PrefArgs& p, int type, hipStream_t s) {
-  const unsigned rows = p.n > 0 ? (unsigned)p.n : 1u;
-  if (type == OT_F32) preference_backward_kernel<OT_F32><<<rows, 256, 0, s>>>(p);
-  else if (type == OT_BF16) preference_backward_kernel<OT_BF16><<<rows, 256, 0, s>>>(p);
-  else preference_backward_kernel<OT_F16><<<rows, 256, 0, s>>>(p);
+  if (type == OT_F32) launch_backward_typed<OT_F32>(p, s);
+  else if (type == OT_BF16) launch_backward_typed<OT_BF16>(p, s);
+  else launch_backward_typed<OT_F16>(p, s);
 }

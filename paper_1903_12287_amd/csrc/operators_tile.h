@@ -60,11 +60,17 @@ struct Operand {
   static_assert(MODE == KC || TYPE == OT_F32 || BX >= 64, "a row of four pairs at least");
   static_assert(BX % (8 * NW) == 0, "whole moves");
 
+  // A wave's moves are alike but for their rows: KC 8 NW apart; KR RSTEP apart, whose swizzle returns every 16 rows.
+  static constexpr int RSTEP = NW * 64 / RS;
+  static constexpr int OFFS = MODE == KC || RSTEP % 16 == 0 ? 1 : 2;
+  static_assert(MODE == KC || RSTEP % 8 == 0, "rows 8 or 16 apart");
+
   const char* base;
   int64_t step;        // bytes from a slice to the next
-  uint32_t off[MOVES];
-  uint32_t kat[MOVES]; // the summed index that a move's lane fetches, in its slice
-  uint32_t kdim;
+  uint32_t ldb;        // bytes from a row to the next
+  uint32_t off[OFFS];  // this lane's 16 bytes in the wave's first moves
+  uint32_t kat, kdim;  // KC: the summed index that they hold, in their slice; its end
+  uint32_t bytes;      // KC: of the rows that exist
   int wave;
 
   __device__ __forceinline__ static int kr_swizzle(int row) {
@@ -77,30 +83,44 @@ struct Operand {
     base = (const char*)p;
     wave = w;
     kdim = (uint32_t)kd;
-    step = MODE == KC ? 128 : (int64_t)KS * ld * ES;
+    ldb = (uint32_t)(ld * ES);
+    step = MODE == KC ? 128 : (int64_t)KS * ldb;
+    if (MODE == KC) {
+      const int x = 8 * w + (lane >> 3), q = (lane & 7) ^ (x & 7);
+      kat = q * EV;
+      off[0] = (uint32_t)x * ldb + 16 * q;
+      bytes = (uint32_t)min(xdim, BX) * ldb;
+    } else {
 #pragma unroll
-    for (int j = 0; j < MOVES; ++j) {
-      const int inst = w + NW * j;
-      if (MODE == KC) {
-        const int x = 8 * inst + (lane >> 3), q = (lane & 7) ^ (x & 7);
-        kat[j] = q * EV;
-        off[j] = x < xdim ? (uint32_t)(x * (uint32_t)(ld * ES) + 16 * q) : pieces::kOob;
-      } else {
-        const int slot = inst * 64 + lane, row = slot / RS, s = slot % RS;
+      for (int v = 0; v < OFFS; ++v) {
+        const int slot = (w + NW * v) * 64 + lane, row = slot / RS, s = slot % RS;
         const int col = TYPE == OT_F32 ? 16 * ((s >> 2) ^ kr_swizzle(row)) + 4 * (s & 3)
                                        : 16 * ((s >> 1) ^ kr_swizzle(row)) + 8 * (s & 1);
-        kat[j] = row;
-        off[j] = col < xdim ? (uint32_t)(row * (uint32_t)(ld * ES) + col * ES) : pieces::kOob;
+        off[v] = col < xdim ? (uint32_t)(row - v * RSTEP) * ldb + col * ES : pieces::kOob;
       }
+      kat = 0;
+      bytes = 0;
     }
   }
 
-  // slice kt into the stage at lds
+  // slice kt into the stage, `at` bytes in.  The buffer's size leaves out the rows past the operand (KC: past its
+  // rows; KR: past the summed index).
   __device__ __forceinline__ void fetch(lds_t* lds, int at, int kt) const {
-    const rsrc_t rs = pieces::make_rsrc(base + kt * step);
+    const char* p = base + kt * step;
+    uint32_t size = bytes;
+    if (MODE == KR) {
+      const int64_t left = (int64_t)kdim - (int64_t)kt * KS;
+      size = left <= 0 ? 0u : (uint32_t)min((int64_t)0x7FFFFFF0, left * ldb);
+    }
+    const uint64_t v = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)(((uint64_t)hi << 32) | lo), (short)0,
+                                                        __builtin_amdgcn_readfirstlane(size), 0x00020000);
+    const bool in = MODE == KR || (uint32_t)kt * KS + kat < kdim;
 #pragma unroll
     for (int j = 0; j < MOVES; ++j) {
-      const uint32_t o = (uint32_t)kt * KS + kat[j] < kdim ? off[j] : pieces::kOob;
+      const uint32_t o = (in ? off[j % OFFS] : pieces::kOob) + (uint32_t)(j * (MODE == KC ? 8 * NW : RSTEP)) * ldb;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (pieces::lds_void*)(lds + (at + (wave + NW * j) * 1024)), 16, o, 0, 0, 0);
     }
   }

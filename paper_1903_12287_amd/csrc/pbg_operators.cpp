@@ -215,7 +215,7 @@ extern "C" pbg_status pbg_group_linear_backward(pbg_ctx* ctx, int32_t dtype, con
     if (da) ops.add(&g.x, &g.ldx, n, in_dim);
     if (dx) ops.add(&g.a, &g.lda, gm, in_dim);
   }
-  if (da) plan_group_da(dtype, n, groups, out_dim, in_dim, &plan);
+  if (da) plan_group_da(n, groups, out_dim, in_dim, &plan);
   st = workspace(ctx, ops.bytes + (size_t)plan.partial_slots * out_dim * in_dim * 4);
   if (st != PBG_OK) return st;
   ops.place((char*)ctx->ops_ws);
@@ -291,7 +291,8 @@ extern "C" pbg_status pbg_preference_loss(pbg_ctx* ctx, int32_t dtype, const voi
       if (overlap(out[i], out[j])) return set_err(ctx, PBG_ERR_INVALID_ARG, "two outputs overlap");
   }
   st = ensure_edge_flags(ctx);
-  if (st == PBG_OK) st = workspace(ctx, (size_t)std::max<int64_t>(n, 1) * 8);
+  const int splits = preference_splits(n, candidates);
+  if (st == PBG_OK) st = workspace(ctx, (size_t)std::max<int64_t>(n, 1) * 8 * std::max(splits, 1));
   if (st != PBG_OK) return st;
   ctx->edge_dirty = true;
   PrefArgs p{};
@@ -310,16 +311,12 @@ extern "C" pbg_status pbg_preference_loss(pbg_ctx* ctx, int32_t dtype, const voi
   p.dlogp = dlogp;
   p.stats = row_stats;
   p.picked = (double*)ctx->ops_ws;
+  p.parts = (float2*)ctx->ops_ws;
+  p.splits = splits;
   p.bad = ctx->edge_flag;
   p.host_bad = ctx->edge_hflag;
-  launch_check_offsets(offsets, 2 * pairs, n, ctx->edge_flag, ctx->cs);
-  launch_check_labels(p, ctx->cs);
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess) {
-    launch_preference_loss(p, dtype, ctx->cs);
-    e = hipGetLastError();
-  }
-  return end_call(ctx, e, "pbg_preference_loss");
+  launch_preference_loss(p, dtype, ctx->cs);
+  return end_call(ctx, hipGetLastError(), "pbg_preference_loss");
 }
 
 extern "C" pbg_status pbg_preference_loss_backward(pbg_ctx* ctx, int32_t dtype, const void* logits, int64_t ld,
@@ -360,14 +357,9 @@ extern "C" pbg_status pbg_preference_loss_backward(pbg_ctx* ctx, int32_t dtype, 
   p.lddl = lddl;
   p.bad = ctx->edge_flag;
   p.host_bad = ctx->edge_hflag;
-  launch_check_offsets(offsets, 2 * pairs, n, ctx->edge_flag, ctx->cs);
-  launch_check_labels(p, ctx->cs);
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess) {
-    launch_preference_backward(p, dtype, ctx->cs);
-    e = hipGetLastError();
-  }
-  return end_call(ctx, e, "pbg_preference_loss_backward");
+  p.splits = 1;
+  launch_preference_backward(p, dtype, ctx->cs);
+  return end_call(ctx, hipGetLastError(), "pbg_preference_loss_backward");
 }
 
 extern "C" pbg_status pbg_clip_gradients(pbg_ctx* ctx, int32_t num_tensors, const int32_t* dtypes_host,
@@ -434,14 +426,7 @@ extern "C" pbg_status pbg_clip_gradients(pbg_ctx* ctx, int32_t num_tensors, cons
     st = workspace(ctx, (size_t)(blocks + 1) * 8);
     if (st != PBG_OK) return st;
     double* scale = (double*)ctx->ops_ws;
-    double* parts = scale + 1;
-    int64_t at = 0;
-    for (const ClipBatch& b : batches) {
-      launch_clip_squares(b, parts + at, ctx->cs);
-      at += b.first[b.n];
-    }
-    launch_clip_factor(parts, blocks, max_norm, scale, ctx->ops_host, ctx->cs);
-    for (const ClipBatch& b : batches) launch_clip_scale(b, scale, ctx->cs);
+    launch_clip(batches.data(), (int)batches.size(), blocks, max_norm, scale, scale + 1, ctx->ops_host, ctx->cs);
     hipError_t e = hipGetLastError();
     const hipError_t es = hipStreamSynchronize(ctx->cs);
     if (e == hipSuccess) e = es;
