@@ -79,7 +79,7 @@ void launch_preference_backward(const PrefArgs& p, int type, hipStream_t s);
 
 // ---- clipping -----------------------------------------------------------------------------------
 constexpr int kClipBatch = 96;          // tensors a launch takes (its arguments hold their descriptors)
-constexpr int kClipBlock = 8192;        // values a workgroup takes
+constexpr int kClipBlock = 8192;        // values a workgroup takes at a time
 
 struct ClipBatch {
   const void* g[kClipBatch];
@@ -88,6 +88,7 @@ struct ClipBatch {
   uint32_t first[kClipBatch + 1];       // first workgroup of each tensor; first[n]: their number
   uint8_t type[kClipBatch];
   int32_t n;
+  int64_t span;                         // values of a workgroup, a multiple of kClipBlock
 };
 
 // all batches: sums of squares into parts (one a workgroup, `blocks` in all), the norm into *host_norm, the scaling

@@ -2,7 +2,7 @@
 // norm = sqrt(sum of all squares), out = g min(1, max_norm / norm).
 //
 // Bound by memory: the gradients are read for the norm, read again and written.  A workgroup takes 8,192 values of one
-// tensor, 16 bytes a load, all of a thread's loads on their way at once; its sum of squares goes to a place of its
+// tensor at a time, 16 bytes a load, all of a thread's loads on their way at once; its sum of squares goes to a place of its
 // own, so the norm does not depend on the order in which workgroups end.  The scaling walks the workgroups backwards:
 // what the norm read last is still in the 256 MB cache beside the memory.  Squares and their sums are float64
 // (an instruction a value: the vector unit keeps up with memory), so the norm neither overflows nor loses small
@@ -21,17 +21,16 @@ __device__ __forceinline__ int tensor_of_block(const ClipBatch& b, uint32_t bloc
     t += __popcll(__ballot(k < b.n && b.first[k < kClipBatch ? k : 0] <= block));
   }
   t = __builtin_amdgcn_readfirstlane(t - 1);
-  at = (int64_t)(block - b.first[t]) * kClipBlock;
+  at = (int64_t)(block - b.first[t]) * b.span;
   return t;
 }
 
 template <int TYPE>
-__device__ __forceinline__ double squares(const void* g, int64_t at, int64_t count) {
+__device__ __forceinline__ void squares(const void* g, int64_t at, int64_t count, double (&s)[4]) {
   typedef typename Elem<TYPE>::T T;
   typedef typename Vec<TYPE>::V V;
   constexpr int N = Vec<TYPE>::N, LOADS = kClipBlock / 256 / N;
   const T* p = (const T*)g + at;
-  double s[4] = {0.0, 0.0, 0.0, 0.0};
   if (count - at >= kClipBlock) {
     V v[LOADS];
 #pragma unroll
@@ -61,7 +60,6 @@ __device__ __forceinline__ double squares(const void* g, int64_t at, int64_t cou
       }
     }
   }
-  return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 template <int TYPE>
@@ -120,10 +118,14 @@ __global__ __launch_bounds__(256) void clip_squares_kernel(ClipBatch b, double* 
   __shared__ double red[4];
   int64_t at;
   const int t = tensor_of_block(b, blockIdx.x, at);
-  const int64_t count = b.count[t];
-  double s = b.type[t] == OT_F32 ? squares<OT_F32>(b.g[t], at, count)
-                                 : (b.type[t] == OT_BF16 ? squares<OT_BF16>(b.g[t], at, count)
-                                                         : squares<OT_F16>(b.g[t], at, count));
+  const int64_t end = min(b.count[t], at + b.span);
+  double p[4] = {0.0, 0.0, 0.0, 0.0};
+  for (; at < end; at += kClipBlock) {
+    if (b.type[t] == OT_F32) squares<OT_F32>(b.g[t], at, end, p);
+    else if (b.type[t] == OT_BF16) squares<OT_BF16>(b.g[t], at, end, p);
+    else squares<OT_F16>(b.g[t], at, end, p);
+  }
+  double s = (p[0] + p[1]) + (p[2] + p[3]);
   s = wave_sum_d(s);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
@@ -175,9 +177,12 @@ __global__ __launch_bounds__(256) void clip_scale_kernel(ClipBatch b, const doub
   int64_t at;
   const int t = tensor_of_block(b, gridDim.x - 1 - blockIdx.x, at);
   if (f == 1.0 && b.o[t] == b.g[t]) return;
-  if (b.type[t] == OT_F32) scale_block<OT_F32>(b.g[t], b.o[t], at, b.count[t], f);
-  else if (b.type[t] == OT_BF16) scale_block<OT_BF16>(b.g[t], b.o[t], at, b.count[t], f);
-  else scale_block<OT_F16>(b.g[t], b.o[t], at, b.count[t], f);
+  const int64_t end = min(b.count[t], at + b.span);
+  for (; at < end; at += kClipBlock) {
+    if (b.type[t] == OT_F32) scale_block<OT_F32>(b.g[t], b.o[t], at, end, f);
+    else if (b.type[t] == OT_BF16) scale_block<OT_BF16>(b.g[t], b.o[t], at, end, f);
+    else scale_block<OT_F16>(b.g[t], b.o[t], at, end, f);
+  }
 }
 
 // Up to so many parts every workgroup of the scaling adds them itself, four loads a thread: a launch less (a small

@@ -108,7 +108,7 @@ __global__ __launch_bounds__(256) void row_stats_kernel(PrefArgs p) {
   const int tid = WAVE ? threadIdx.x & 63 : threadIdx.x;
   if (t >= p.n) return;
   const int label = p.labels[t];
-  if (sequence_of_row(p.offsets, 2 * p.pairs, t) < 0) return;
+  if (t < p.offsets[0] || t >= p.offsets[2 * p.pairs]) return;   // which sequence it is does not matter here
   if (label < 0) {
     if (tid == 0) {
       p.stats[2 * t] = p.stats[2 * t + 1] = 0.0f;
@@ -174,8 +174,15 @@ __global__ __launch_bounds__(1024) void pair_loss_kernel(PrefArgs p) {
         if (label >= 0) {
           const Stats* q = (const Stats*)p.parts + t * p.splits;
           const float z_label = (float)((const T*)p.logits)[t * p.ld + label];
-          Stats a = q[0];
-          for (int i = 1; i < p.splits; ++i) join<TYPE>(a, q[i]);
+          Stats a = {-INFINITY, 0.0f};
+          for (int i0 = 0; i0 < p.splits; i0 += 8) {   // eight loads on their way at a time
+            Stats b[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] = q[min(i0 + i, p.splits - 1)];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (i0 + i < p.splits) join<TYPE>(a, b[i]);
+          }
           finish_row(a, z_label, st, l);
         }
         p.stats[2 * t] = st.x;

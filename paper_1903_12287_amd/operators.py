@@ -168,17 +168,21 @@ def pbg_clip_gradients(ctx, grads, max_norm, outs=None) -> float:
     n = len(grads)
     if outs is not None and len(outs) != n:
         raise ValueError("one output per gradient")
-    gp, op = (ctypes.c_void_p * max(n, 1))(), (ctypes.c_void_p * max(n, 1))()
-    counts, types = (ctypes.c_int64 * max(n, 1))(), (ctypes.c_int32 * max(n, 1))()
     for i, g in enumerate(grads):
         dt = _type(g, f"grads[{i}]")
-        gp[i] = pbg._ptr(g, dt, f"grads[{i}]")
-        counts[i], types[i] = g.numel(), TYPES[dt]
+        if not (g.is_cuda and g.is_contiguous()):
+            pbg._ptr(g, dt, f"grads[{i}]")   # raises
         if outs is not None:
-            if isinstance(outs[i], torch.Tensor) and outs[i].shape != g.shape:
-                raise ValueError(f"outs[{i}] must be {tuple(g.shape)}, got {tuple(outs[i].shape)}")
-            op[i] = pbg._ptr(outs[i], dt, f"outs[{i}]")
+            o = outs[i]
+            if not (isinstance(o, torch.Tensor) and o.dtype == dt and o.is_cuda and o.is_contiguous()):
+                pbg._ptr(o, dt, f"outs[{i}]")
+            if o.shape != g.shape:
+                raise ValueError(f"outs[{i}] must be {tuple(g.shape)}, got {tuple(o.shape)}")
+    m = max(n, 1)
+    gp = (ctypes.c_void_p * m)(*[g.data_ptr() for g in grads])
+    op = None if outs is None else (ctypes.c_void_p * m)(*[o.data_ptr() for o in outs])
+    counts = (ctypes.c_int64 * m)(*[g.numel() for g in grads])
+    types = (ctypes.c_int32 * m)(*[TYPES[g.dtype] for g in grads])
     norm = ctypes.c_double(0.0)
-    _check(ctx, library().pbg_clip_gradients(ctx, n, types, counts, gp, None if outs is None else op, float(max_norm),
-                                             ctypes.byref(norm)))
+    _check(ctx, library().pbg_clip_gradients(ctx, n, types, counts, gp, op, float(max_norm), ctypes.byref(norm)))
     return norm.value
