@@ -41,35 +41,67 @@ __device__ __forceinline__ void join(Stats& a, const Stats& b) {
   a.m = m;
 }
 
-// values [first, last) of a row by THREADS threads, U loads of 16 bytes on their way at a time
+// Scores of 16 bits take exp(x - m) as 2^(x log2(e) - M), M = m log2(e) rounded: one multiply-add, exact but for its
+// own rounding; what M's rounding and log2(e)'s left out is the same for every term and comes off the sum.  Far from
+// zero (where that would no longer be small) and in float32 the difference is formed first.
+template <int TYPE, int COUNT>
+__device__ __forceinline__ void add_scores(Stats& a, const float (&x)[COUNT]) {
+  float m = a.m;
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i) m = fmaxf(m, x[i]);
+  const float base = base_of(m);
+  const float old = a.s * exp_of<TYPE>(a.m - base);
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (TYPE != OT_F32 && fabsf(base) < 65536.0f * 16.0f) {
+    constexpr float L = 1.44269502f;
+    const float M = base * L;
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) s[i & 3] += __builtin_amdgcn_exp2f(fmaf(x[i], L, -M));
+    const float left = fmaf(base, L, -M);   // exact
+    a.s = fmaf((s[0] + s[1]) + (s[2] + s[3]), __builtin_amdgcn_exp2f(-left), old);
+  } else {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) s[i & 3] += exp_of<TYPE>(x[i] - base);
+    a.s = old + ((s[0] + s[1]) + (s[2] + s[3]));
+  }
+  a.m = m;
+}
+
+// values [first, last) of a row by THREADS threads, U loads of 16 bytes on their way at a time, and the next U while
+// they are added
 template <int TYPE, int THREADS>
 __device__ __forceinline__ Stats scan(const typename Elem<TYPE>::T* z, int first, int last, int tid) {
   typedef typename Vec<TYPE>::V V;
-  constexpr int N = Vec<TYPE>::N, U = 4;
+  constexpr int N = Vec<TYPE>::N, U = 4, STEP = THREADS * N * U;
   Stats a = {-INFINITY, 0.0f};
-  for (int v0 = first; v0 < last; v0 += THREADS * N * U) {
+  if (last - first < N) {
+    const float y[1] = {first + tid < last ? (float)z[first + tid] : -INFINITY};
+    add_scores<TYPE>(a, y);
+  } else {
+    // 16 bytes that would reach past the end are taken from before it, so that no load is behind a branch; what they
+    // hold twice counts for nothing
+    auto load = [&](V (&w)[U], int v0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) w[u] = *(const V*)(z + min(v0 + (u * THREADS + tid) * N, last - N));
+    };
     float x[U * N];
+    V w[U], next[U];
+    load(w, first);
+    int v0 = first;
+    for (; v0 + STEP < last; v0 += STEP) {   // every value of w counts, and more are left
+      load(next, v0 + STEP);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int v = v0 + (u * THREADS + tid) * N;
-      if (v + N <= last) {
-        const V w = *(const V*)(z + v);
+      for (int i = 0; i < U * N; ++i) x[i] = (float)w[i / N][i % N];
+      add_scores<TYPE>(a, x);
 #pragma unroll
-        for (int j = 0; j < N; ++j) x[u * N + j] = (float)w[j];
-      } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) x[u * N + j] = v + j < last ? (float)z[v + j] : -INFINITY;
-      }
+      for (int u = 0; u < U; ++u) w[u] = next[u];
     }
-    float m = a.m;
 #pragma unroll
-    for (int i = 0; i < U * N; ++i) m = fmaxf(m, x[i]);
-    const float base = base_of(m);
-    float s[4] = {a.s * exp_of<TYPE>(a.m - base), 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < U * N; ++i) s[i & 3] += exp_of<TYPE>(x[i] - base);
-    a.m = m;
-    a.s = (s[0] + s[1]) + (s[2] + s[3]);
+    for (int i = 0; i < U * N; ++i) {
+      const int v = v0 + (i / N * THREADS + tid) * N;
+      x[i] = v + N <= last || last - N + i % N >= v ? (float)w[i / N][i % N] : -INFINITY;
+    }
+    add_scores<TYPE>(a, x);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {

@@ -63,24 +63,41 @@ def _type(t, what):
 
 def _rows(t, dtype, shape, what):
     """Pointer and row stride of a device matrix whose columns are consecutive."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{what} must be a torch.Tensor")
-    if t.dtype != dtype:
-        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.device.type != "cuda":
-        raise ValueError(f"{what} must be a device tensor")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what} must be {tuple(shape)}, got {tuple(t.shape)}")
     n, width = shape
-    if width > 1 and t.stride(1) != 1:
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_cuda and t.shape == shape
+            and (width <= 1 or t.stride(1) == 1)):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{what} must be a torch.Tensor")
+        if t.dtype != dtype:
+            raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+        if not t.is_cuda:
+            raise ValueError(f"{what} must be a device tensor")
+        if t.shape != shape:
+            raise ValueError(f"{what} must be {shape}, got {tuple(t.shape)}")
         raise ValueError(f"{what} must have consecutive columns")
-    return (ctypes.c_void_p(t.data_ptr()) if t.numel() else None), (t.stride(0) if n > 1 else max(width, 1))
+    return (t.data_ptr() if n and width else None), (t.stride(0) if n > 1 else max(width, 1))
 
 
 def _vector(t, dtype, n, what, allow_none=False):
+    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_cuda and t.is_contiguous() and t.numel() == n:
+        return t.data_ptr() if n else None
     if t is not None and isinstance(t, torch.Tensor) and t.numel() != n:
         raise ValueError(f"{what} must hold {n} values, got {t.numel()}")
     return pbg._ptr(t, dtype, what, allow_none=allow_none)
+
+
+def _values(tensors, what):
+    """Types, numbers of values and pointers of contiguous device tensors of any shapes (an attribute at a time over
+    all of them: half the time of a loop over tensors)."""
+    try:
+        types = [TYPES[t.dtype] for t in tensors]
+        if all([t.is_cuda for t in tensors]) and all([t.is_contiguous() for t in tensors]):
+            return types, [t.numel() for t in tensors], [t.data_ptr() for t in tensors]
+    except (KeyError, AttributeError):
+        pass
+    for i, t in enumerate(tensors):   # which one, and why
+        pbg._ptr(t, _type(t, f"{what}[{i}]"), f"{what}[{i}]")
+    raise TypeError(f"{what} must be tensors")
 
 
 def _matrices(a, dtype, what):
@@ -163,26 +180,20 @@ def pbg_preference_loss_backward(ctx, logits, labels, offsets, row_stats, dlogp,
 
 
 def pbg_clip_gradients(ctx, grads, max_norm, outs=None) -> float:
-    """grads: tensors of any shapes (contiguous; float32, bfloat16, float16 mixed); outs: tensors like them, or None to
-    scale in place.  Returns the joint norm before the scaling."""
+    """grads: tensors of any shapes (contiguous; float32, bfloat16, float16 mixed); outs: as many tensors of their types and
+    sizes, or None to scale in place.  Returns the joint norm before the scaling."""
     n = len(grads)
     if outs is not None and len(outs) != n:
         raise ValueError("one output per gradient")
-    for i, g in enumerate(grads):
-        dt = _type(g, f"grads[{i}]")
-        if not (g.is_cuda and g.is_contiguous()):
-            pbg._ptr(g, dt, f"grads[{i}]")   # raises
-        if outs is not None:
-            o = outs[i]
-            if not (isinstance(o, torch.Tensor) and o.dtype == dt and o.is_cuda and o.is_contiguous()):
-                pbg._ptr(o, dt, f"outs[{i}]")
-            if o.shape != g.shape:
-                raise ValueError(f"outs[{i}] must be {tuple(g.shape)}, got {tuple(o.shape)}")
+    types, counts, gp = _values(grads, "grads")
+    op = None
+    if outs is not None:
+        otypes, ocounts, op = _values(outs, "outs")
+        if otypes != types or ocounts != counts:
+            raise ValueError("every output must have its gradient's type and number of values")
     m = max(n, 1)
-    gp = (ctypes.c_void_p * m)(*[g.data_ptr() for g in grads])
-    op = None if outs is None else (ctypes.c_void_p * m)(*[o.data_ptr() for o in outs])
-    counts = (ctypes.c_int64 * m)(*[g.numel() for g in grads])
-    types = (ctypes.c_int32 * m)(*[TYPES[g.dtype] for g in grads])
+    types, counts = (ctypes.c_int32 * m)(*types), (ctypes.c_int64 * m)(*counts)
+    gp, op = (ctypes.c_void_p * m)(*gp), None if op is None else (ctypes.c_void_p * m)(*op)
     norm = ctypes.c_double(0.0)
     _check(ctx, library().pbg_clip_gradients(ctx, n, types, counts, gp, op, float(max_norm), ctypes.byref(norm)))
     return norm.value
