@@ -12,9 +12,6 @@ inline int type_bytes(int type) { return type == OT_F32 ? 4 : 2; }
 // bits of the device-side argument checks
 enum { OPS_BAD_OFFSETS = 1, OPS_BAD_LABEL = 2 };
 
-// offsets[0..groups] nondecreasing and within [0, n], else OPS_BAD_OFFSETS into *flag
-void launch_check_offsets(const int64_t* offsets, int groups, int64_t n, uint32_t* flag, hipStream_t s);
-
 // ---- grouped products ---------------------------------------------------------------------------
 enum { GP_FORWARD = 0, GP_DX = 1, GP_DA = 2 };
 
@@ -34,13 +31,26 @@ struct GroupArgs {
   uint32_t* host_bad;   // receives it where it is not 0
 };
 
-struct GroupPlan {
-  int da_shift;            // da: rows of a slot, 2^da_shift
-  int64_t partial_slots;   // slots of partial sums, m k floats each (0: no group is longer than a slot)
-  float* partial;
+// A slot is 2^shift rows of one group, or fewer at its end, or none.
+struct GroupSlots {
+  int shift;
+  int64_t count;   // slots: n / 2^shift + groups
+  int4* at;        // workspace: {first row, rows, group or -1, da: place of its partial sum or -1}
 };
 
-void plan_group_da(int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p);
+struct GroupPlan {
+  GroupSlots rows;         // y, dx: a slot's rows are a tile's
+  GroupSlots da;           // da: a slot's rows are summed by one workgroup
+  int64_t partial_slots;   // places of partial sums, m k floats each (0: no group is longer than a slot)
+  float* partial;
+  int2* join;              // [partial_slots]: {group whose first sum this is or -1, number of sums}
+  size_t bytes() const { return (size_t)(rows.count + da.count) * 16 + (size_t)partial_slots * 8; }
+};
+
+// what the call needs (count 0: not wanted), for workspace and launches
+GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int64_t k, bool want_da);
+// the tables of slots, and offsets[0..groups] nondecreasing and within [0, n], else OPS_BAD_OFFSETS into *flag
+void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, int64_t n, uint32_t* flag, hipStream_t s);
 // up to three operands into rows of wp values, a multiple of 16 bytes, zeros behind `width`
 void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,
                        const int64_t* rows, const int* width, const int* wp, hipStream_t s);

@@ -32,31 +32,6 @@ __device__ __forceinline__ bool args_good(const uint32_t* bad, uint32_t* host_ba
   return v == 0;
 }
 
-// Rows cut into blocks of 2^shift that never straddle two groups, without a table: group g's blocks take the
-// slots from offsets[g] / 2^shift + g on.  A group of L rows needs ceil(L / 2^shift) slots and has
-// floor(end / 2^shift) - floor(start / 2^shift) + 1 of them, which is never less; n / 2^shift + groups slots hold
-// every block, and those left over are empty.
-__device__ __forceinline__ int64_t first_slot(const int64_t* offsets, int g, int shift) {
-  return (offsets[g] >> shift) + g;
-}
-
-// the last group whose first slot is at most `slot`, or -1; the wave's 64 lanes probe together, so 64 groups take
-// one round trip to memory and 2^18 take three
-__device__ __forceinline__ int group_of_slot(const int64_t* offsets, int groups, int shift, int64_t slot) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, hi = groups;
-  while (true) {
-    const int step = (hi - lo + 63) >> 6;
-    const int g = lo + lane * step;
-    const bool in = g < hi && first_slot(offsets, g, shift) <= slot;
-    const int c = __popcll(__ballot(in));
-    if (c == 0) return -1;
-    lo += (c - 1) * step;
-    if (step == 1) return __builtin_amdgcn_readfirstlane(lo);
-    hi = min(hi, lo + step);
-  }
-}
-
 // the sequence that holds row t: the last one with offsets[q] <= t < offsets[q + 1] (empty ones in front of it share
 // its start), or -1
 __device__ __forceinline__ int sequence_of_row(const int64_t* offsets, int sequences, int64_t t) {

@@ -2,8 +2,10 @@
 //   forward  y[t, :]  = A_g x[t, :]                over in_dim
 //   dx       dx[t, :] = A_g^T dy[t, :]             over out_dim
 //   da       dA_g     = sum_t dy[t, :] x[t, :]^T   over the group's rows
-// The host does not know the groups' sizes: a workgroup finds its group and rows from the offsets alone
-// (group_of_slot), so a call needs neither a table nor a wait before its product.
+// The host does not know the groups' sizes, so it launches a workgroup for every slot of rows that there could be, and
+// a kernel ahead of the products (which also checks the offsets) writes down which group and rows a slot is.  (Every
+// workgroup searching the offsets itself: four loads one behind the other before its first fetch, 2.5 of the 10 us of
+// a workgroup with 32 rows of 400.)
 #include <algorithm>
 
 #include "operators_tile.h"
@@ -14,11 +16,13 @@ using tile::KC;
 using tile::KR;
 
 struct Launch {
-  int shift;              // rows of a slot: 2^shift
+  const int4* slots;
+  int shift;                  // da: rows of a slot: 2^shift
   int row_tiles, col_tiles;   // da: tiles of one matrix; y, dx: slots of all groups, tiles of the columns
   uint32_t blocks;
-  bool vec;               // rows of the output start at multiples of four values
-  float* partial;         // da: partial sums of the groups of several slots
+  bool vec;                   // rows of the output start at multiples of four values
+  float* partial;             // da: partial sums of the groups of several slots
+  const int2* join;
 };
 
 // Tiles in bands of BAND slots, column by column: the workgroups that an XCD runs at a time share the rows of a few
@@ -38,15 +42,15 @@ __global__ __launch_bounds__(64 * WM * WN) void group_rows_kernel(GroupArgs g, L
   constexpr int ES = TYPE == OT_F32 ? 4 : 2;
   constexpr int BAND = BM >= 256 ? 4 : 8;
   __shared__ __attribute__((aligned(1024))) char lds0[Tl::STAGE], lds1[Tl::STAGE];
-  if (!args_good(g.bad, g.host_bad)) return;
-  const uint32_t at = tile::xcd_place(blockIdx.x, L.blocks);
+  // Few rows a matrix: little is shared, and the XCDs are kept even by taking the tiles in turn.
+  const uint32_t at = BM >= 128 ? tile::xcd_place(blockIdx.x, L.blocks) : blockIdx.x;
   uint32_t slot, col;
   band_tile<BAND>(at, L.row_tiles, L.col_tiles, slot, col);
   const int j0 = (int)col * BN;
-  const int grp = group_of_slot(g.offsets, g.groups, L.shift, slot);
-  if (grp < 0) return;
-  const int64_t r0 = g.offsets[grp] + (((int64_t)slot - first_slot(g.offsets, grp, L.shift)) << L.shift);
-  const int rows = (int)min((int64_t)BM, g.offsets[grp + 1] - r0);
+  const int4 at_slot = L.slots[slot];
+  if (!args_good(g.bad, g.host_bad)) return;
+  const int64_t r0 = at_slot.x;
+  const int rows = at_slot.y, grp = at_slot.z;
   if (rows <= 0) return;
   const char* a = (const char*)g.a + grp * g.a_group * ES;
   v4f acc[Tl::IB][Tl::JB];
@@ -59,38 +63,29 @@ __global__ __launch_bounds__(64 * WM * WN) void group_rows_kernel(GroupArgs g, L
 }
 
 // da: one slot of a group's rows, one tile of its matrix.  A group of one slot is stored; the slots of a longer one
-// leave float32 sums, which group_join_kernel adds in their order.  Group g's slots of partial sums start at
-// floor(2 offsets[g] / 2^shift): a group of L > 2^shift rows has at least ceil(L / 2^shift) of them.
-__device__ __forceinline__ int64_t first_partial(const int64_t* offsets, int g, int shift) {
-  return (2 * offsets[g]) >> shift;
-}
-
+// leave float32 sums, which group_join_kernel adds in their order.
 template <int TYPE, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Launch L) {
   typedef tile::Tile<TYPE, KR, KR, BM, BN, WM, WN> Tl;
   constexpr int ES = TYPE == OT_F32 ? 4 : 2;
   __shared__ __attribute__((aligned(1024))) char lds0[Tl::STAGE], lds1[Tl::STAGE];
-  if (!args_good(g.bad, g.host_bad)) return;
   const uint32_t at = tile::xcd_place(blockIdx.x, L.blocks);
   const int tiles = L.row_tiles * L.col_tiles;
-  const int64_t slot = at / tiles;
+  const int4 slot = L.slots[at / tiles];
   const int t = (int)(at % tiles);
   const int i0 = t / L.col_tiles * BM, j0 = t % L.col_tiles * BN;
-  const int grp = group_of_slot(g.offsets, g.groups, L.shift, slot);
-  if (grp < 0) return;
-  const int64_t first = g.offsets[grp], last = g.offsets[grp + 1];
-  const int64_t part = slot - first_slot(g.offsets, grp, L.shift);
-  const int64_t r0 = first + (part << L.shift);
-  if (part > 0 && r0 >= last) return;   // slot 0 of an empty group stores zeros
-  const int64_t depth = min((int64_t)1 << L.shift, last - r0);
+  if (!args_good(g.bad, g.host_bad)) return;
+  if (slot.z < 0) return;   // the first slot of an empty group stores zeros
+  const int64_t r0 = slot.x, depth = slot.y;
+  const int grp = slot.z;
   v4f acc[Tl::IB][Tl::JB];
   Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.dy + (r0 * g.lddy + i0) * ES, g.lddy, g.md - i0, (const char*)g.x + (r0 * g.ldx + j0) * ES,
           g.ldx, g.kd - j0, depth, acc);
   const int rows = min(BM, g.m - i0), cols = g.k - j0;
-  if (last - first <= (int64_t)1 << L.shift) {
+  if (slot.w < 0) {
     Tl::template store<TYPE>(acc, (char*)g.out + (((int64_t)grp * g.m + i0) * g.k + j0) * ES, g.k, rows, cols, L.vec);
   } else {
-    float* p = L.partial + (first_partial(g.offsets, grp, L.shift) + part) * g.m * g.k;
+    float* p = L.partial + (int64_t)slot.w * g.m * g.k;
     Tl::template store<OT_F32>(acc, p + (int64_t)i0 * g.k + j0, g.k, rows, cols, (g.k & 3) == 0);
   }
 }
@@ -103,24 +98,12 @@ __global__ __launch_bounds__(256) void group_join_kernel(GroupArgs g, Launch L) 
   typedef typename Elem<TYPE>::T T;
   __shared__ float sums[4][64];
   if (!args_good(g.bad, g.host_bad)) return;
-  // first_partial(grp) <= slot; a group of several slots holds two partial slots at least, so at its first one it is
-  // the last group that starts there or before
   const int64_t slot = blockIdx.y;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int lo = 0, hi = g.groups;
-  while (true) {
-    const int step = (hi - lo + 63) >> 6;
-    const int q = lo + lane * step;
-    const int c = __popcll(__ballot(q < hi && first_partial(g.offsets, q, L.shift) <= slot));
-    if (c == 0) return;
-    lo += (c - 1) * step;
-    if (step == 1) break;
-    hi = min(hi, lo + step);
-  }
-  const int grp = __builtin_amdgcn_readfirstlane(lo);
-  const int64_t rows = g.offsets[grp + 1] - g.offsets[grp];
-  if (first_partial(g.offsets, grp, L.shift) != slot || rows <= (int64_t)1 << L.shift) return;
-  const int parts = (int)((rows + ((int64_t)1 << L.shift) - 1) >> L.shift);
+  const int2 at = L.join[slot];
+  if (at.x < 0) return;
+  const int64_t grp = at.x;
+  const int parts = at.y;
   const int per = (parts + 3) >> 2, i0 = w * per, i1 = min(parts, i0 + per);
   const int64_t mk = (int64_t)g.m * g.k;
   const float* p = L.partial + slot * mk;
@@ -173,94 +156,161 @@ __global__ __launch_bounds__(256) void group_pack_kernel(PackArgs a) {
 int64_t tiles_of(int64_t v, int b) { return (v + b - 1) / b; }
 
 template <int TYPE, int WHICH, int BM, int BN, int WM, int WN>
-bool launch_rows(const GroupArgs& g, Launch L, hipStream_t s) {
-  L.shift = __builtin_ctz(BM);
-  const int64_t slots = (g.n >> L.shift) + g.groups;
-  L.row_tiles = (int)slots;
+bool launch_rows(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) {
+  L.slots = p.rows.at;
+  L.row_tiles = (int)p.rows.count;
   L.col_tiles = (int)tiles_of(WHICH == GP_FORWARD ? g.m : g.k, BN);
-  const int64_t blocks = slots * L.col_tiles;
+  const int64_t blocks = p.rows.count * L.col_tiles;
   if (blocks * 64 * WM * WN >= 1ll << 32) return false;
   L.blocks = (uint32_t)blocks;
   group_rows_kernel<TYPE, WHICH, BM, BN, WM, WN><<<L.blocks, 64 * WM * WN, 0, s>>>(g, L);
   return true;
 }
 
-template <int TYPE, int BM, int BN, int WM, int WN>
-bool launch_da(const GroupArgs& g, Launch L, hipStream_t s) {
-  L.row_tiles = (int)tiles_of(g.m, BM);
-  L.col_tiles = (int)tiles_of(g.k, BN);
-  const int64_t blocks = ((g.n >> L.shift) + g.groups) * L.row_tiles * L.col_tiles;
-  if (blocks * 64 * WM * WN >= 1ll << 32) return false;
+template <int TYPE>
+bool launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) {
+  L.slots = p.da.at;
+  L.shift = p.da.shift;
+  L.partial = p.partial;
+  L.join = p.join;
+  L.row_tiles = (int)tiles_of(g.m, 128);
+  L.col_tiles = (int)tiles_of(g.k, 128);
+  const int64_t blocks = p.da.count * L.row_tiles * L.col_tiles;
+  if (blocks * 256 >= 1ll << 32) return false;
   L.blocks = (uint32_t)blocks;
-  group_da_kernel<TYPE, BM, BN, WM, WN><<<L.blocks, 64 * WM * WN, 0, s>>>(g, L);
+  group_da_kernel<TYPE, 128, 128, 2, 2><<<L.blocks, 256, 0, s>>>(g, L);
+  if (p.partial_slots > 0) {
+    const dim3 grid((unsigned)std::min<int64_t>(tiles_of((int64_t)g.m * g.k, 64), 4096), (unsigned)p.partial_slots);
+    group_join_kernel<TYPE><<<grid, 256, 0, s>>>(g, L);
+  }
   return true;
 }
 
+// Rows of a tile of y or dx, 2^shift, by the average group.  A tile as tall as its group reads the group's matrix once
+// and multiplies few rows that are not there; of 256 x 256 the forward product of 16 bits does a third more a second
+// than of 128 x 128, where there are tiles enough for the 256 compute units (dx, whose matrix is read through the
+// transposing LDS read, runs out of registers there).
+int row_shift(int type, int which, int64_t n, int groups, int64_t cols) {
+  const int64_t average = n / groups;
+  if (type != OT_F32 && which == GP_FORWARD && average >= 256 && n / 256 * tiles_of(cols, 256) >= 256) return 8;
+  return average >= 64 ? 7 : 5;
+}
+
 template <int TYPE, int WHICH>
-bool launch_rows_by_size(const GroupArgs& g, const Launch& L, hipStream_t s) {
-  const int64_t cols = WHICH == GP_FORWARD ? g.m : g.k;
-  const int64_t average = g.n / g.groups;
-  if constexpr (TYPE != OT_F32) {
-    if (average >= 256 && g.n / 256 * tiles_of(cols, 256) >= 256)
-      return launch_rows<TYPE, WHICH, 256, 256, 2, 4>(g, L, s);
+bool launch_rows_by_size(const GroupArgs& g, const GroupPlan& p, const Launch& L, hipStream_t s) {
+  if constexpr (TYPE != OT_F32 && WHICH == GP_FORWARD) {
+    if (p.rows.shift == 8) return launch_rows<TYPE, WHICH, 256, 256, 2, 4>(g, p, L, s);
   }
-  if (average >= 64) return launch_rows<TYPE, WHICH, 128, 128, 2, 2>(g, L, s);
-  return launch_rows<TYPE, WHICH, 32, 128, 1, 4>(g, L, s);
+  if (p.rows.shift == 7) return launch_rows<TYPE, WHICH, 128, 128, 2, 2>(g, p, L, s);
+  return launch_rows<TYPE, WHICH, 32, 128, 1, 4>(g, p, L, s);
 }
 
 template <int TYPE>
 bool launch_typed(const GroupArgs& g, int which, const GroupPlan& p, hipStream_t s) {
   Launch L{};
   L.vec = g.ldo % 4 == 0 && ((uintptr_t)g.out & (TYPE == OT_F32 ? 15 : 7)) == 0;
-  if (which == GP_DA) {
-    L.shift = p.da_shift;
-    L.partial = p.partial;
-    if (!launch_da<TYPE, 128, 128, 2, 2>(g, L, s)) return false;
-    if (p.partial_slots > 0) {
-      const int64_t mk = (int64_t)g.m * g.k;
-      const dim3 grid((unsigned)std::min<int64_t>(tiles_of(mk, 64), 4096), (unsigned)p.partial_slots);
-      group_join_kernel<TYPE><<<grid, 256, 0, s>>>(g, L);
-    }
-    return true;
-  }
-  if (which == GP_FORWARD) return launch_rows_by_size<TYPE, GP_FORWARD>(g, L, s);
-  return launch_rows_by_size<TYPE, GP_DX>(g, L, s);
+  if (which == GP_DA) return launch_da<TYPE>(g, p, L, s);
+  if (which == GP_FORWARD) return launch_rows_by_size<TYPE, GP_FORWARD>(g, p, L, s);
+  return launch_rows_by_size<TYPE, GP_DX>(g, p, L, s);
 }
 
-__global__ __launch_bounds__(256) void check_offsets_kernel(const int64_t* offsets, int groups, int64_t n,
-                                                            uint32_t* flag) {
+// ---- the tables of slots ---------------------------------------------------------------------------
+// Rows cut into slots of 2^shift that never straddle two groups: group g's slots start at
+// floor(offsets[g] / 2^shift) + g.  A group of L rows needs ceil(L / 2^shift) of them and has
+// floor(end / 2^shift) - floor(start / 2^shift) + 1, which is never less; n / 2^shift + groups slots hold every group.
+// A group's places for partial sums start at floor(2 offsets[g] / 2^shift): one of L > 2^shift rows has at least
+// ceil(L / 2^shift) of them, so that 2 n / 2^shift places are enough, however many groups there are.
+__device__ __forceinline__ int64_t first_slot(int64_t offset, int g, int shift) { return (offset >> shift) + g; }
+__device__ __forceinline__ int64_t first_place(int64_t offset, int shift) { return (2 * offset) >> shift; }
+
+// the last group whose first slot (PLACE: first place) is at most v, or -1
+template <bool PLACE>
+__device__ __forceinline__ int group_at(const int64_t* offsets, int groups, int shift, int64_t v) {
+  int lo = -1, hi = groups;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    const int64_t o = offsets[mid];
+    if ((PLACE ? first_place(o, shift) : first_slot(o, mid, shift)) <= v) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ int4 slot_of(const int64_t* offsets, int groups, int shift, int64_t v, bool places) {
+  const int g = group_at<false>(offsets, groups, shift, v);
+  if (g < 0) return make_int4(0, 0, -1, -1);
+  const int64_t first = offsets[g], last = offsets[g + 1];
+  const int64_t part = v - first_slot(first, g, shift), r0 = first + (part << shift);
+  if (part > 0 && r0 >= last) return make_int4(0, 0, -1, -1);
+  const int64_t rows = min((int64_t)1 << shift, last - r0);
+  const bool several = places && last - first > (int64_t)1 << shift;
+  return make_int4((int)r0, (int)rows, g, several ? (int)(first_place(first, shift) + part) : -1);
+}
+
+// Offsets that are not in order are found here; what the tables then hold is not used.
+__global__ __launch_bounds__(256) void group_plan_kernel(GroupPlan p, const int64_t* offsets, int groups, int64_t n,
+                                                         uint32_t* flag) {
+  const int64_t total = p.rows.count + p.da.count + p.partial_slots;
+  const int64_t step = (int64_t)gridDim.x * 256;
   bool bad = false;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i <= groups; i += (int64_t)gridDim.x * 256) {
-    const int64_t v = offsets[i];
-    bad |= v < 0 || v > n || (i < groups && offsets[i + 1] < v);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total || i <= groups; i += step) {
+    if (i <= groups) {
+      const int64_t v = offsets[i];
+      bad |= v < 0 || v > n || (i < groups && offsets[i + 1] < v);
+    }
+    int64_t v = i;
+    if (v < p.rows.count) {
+      p.rows.at[v] = slot_of(offsets, groups, p.rows.shift, v, false);
+      continue;
+    }
+    v -= p.rows.count;
+    if (v < p.da.count) {
+      p.da.at[v] = slot_of(offsets, groups, p.da.shift, v, true);
+      continue;
+    }
+    v -= p.da.count;
+    if (v < p.partial_slots) {
+      // a group of several slots holds two places at least, so at its first one it is the last group that starts there
+      // or before
+      const int g = group_at<true>(offsets, groups, p.da.shift, v);
+      int2 at = make_int2(-1, 0);
+      if (g >= 0 && first_place(offsets[g], p.da.shift) == v) {
+        const int64_t rows = offsets[g + 1] - offsets[g];
+        if (rows > (int64_t)1 << p.da.shift) at = make_int2(g, (int)((rows + ((int64_t)1 << p.da.shift) - 1) >> p.da.shift));
+      }
+      p.join[v] = at;
+    }
   }
   if (__ballot(bad) && (threadIdx.x & 63) == 0) atomicOr(flag, (uint32_t)OPS_BAD_OFFSETS);
 }
 
 }  // namespace
 
-void launch_check_offsets(const int64_t* offsets, int groups, int64_t n, uint32_t* flag, hipStream_t s) {
-  const int blocks = (groups + 256) / 256;
-  check_offsets_kernel<<<blocks < 1024 ? blocks : 1024, 256, 0, s>>>(offsets, groups, n, flag);
+void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, int64_t n, uint32_t* flag, hipStream_t s) {
+  const int64_t work = std::max<int64_t>(p.rows.count + p.da.count + p.partial_slots, groups + 1);
+  group_plan_kernel<<<(unsigned)std::min<int64_t>(tiles_of(work, 256), 65536), 256, 0, s>>>(p, offsets, groups, n, flag);
 }
 
-void plan_group_da(int64_t n, int groups, int64_t m, int64_t k, GroupPlan* p) {
-  // Rows of a slot: enough slots for a few workgroups on each of the 256 compute units, where the matrices' tiles
+GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int64_t k, bool want_da) {
+  GroupPlan p{};
+  if (which != GP_DA) {
+    p.rows.shift = row_shift(type, which, n, groups, which == GP_FORWARD ? m : k);
+    p.rows.count = (n >> p.rows.shift) + groups;
+  }
+  if (!want_da) return p;
+  // Rows of a slot of da: enough slots for a few workgroups on each of the 256 compute units, where the matrices' tiles
   // alone are not; with tiles enough, only groups of four times the average and more are cut.
   const int64_t tiles = tiles_of(m, 128) * tiles_of(k, 128);
   int64_t rows = std::max<int64_t>(256, n * tiles / 1024);
   if (groups * tiles >= 512) rows = std::max(rows, 4 * n / groups);
   int shift = 8;
   while (shift < 31 && ((int64_t)1 << shift) < rows) ++shift;
-  // the partial sums stay below 512 MB
-  while (shift < 31 && ((2 * n) >> shift) * m * k * 4 > (512ll << 20)) ++shift;
-  p->da_shift = shift;
-  p->partial_slots = n > (int64_t)1 << shift ? (2 * n) >> shift : 0;
-  // a grid has 65,535 slots
-  while (p->partial_slots > 65535) {
-    p->da_shift = ++shift;
-    p->partial_slots = n > (int64_t)1 << shift ? (2 * n) >> shift : 0;
-  }
+  // the partial sums stay below 512 MB, and a grid has 65,535 of them
+  while (shift < 31 && (((2 * n) >> shift) * m * k * 4 > (512ll << 20) || (2 * n) >> shift > 65535)) ++shift;
+  p.da.shift = shift;
+  p.da.count = (n >> shift) + groups;
+  p.partial_slots = n > (int64_t)1 << shift ? (2 * n) >> shift : 0;
+  return p;
 }
 
 void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,

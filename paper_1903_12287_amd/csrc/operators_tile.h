@@ -26,22 +26,22 @@ typedef __attribute__((address_space(3))) char lds_t;   // LDS by its own addres
 template <int TYPE> struct Mfma;
 template <> struct Mfma<OT_F32> {
   typedef v4f Frag;          // four k of one row: k = 4 (lane / 16) + 0..3 of 16
-  static constexpr int STEPS = 2;
-  __device__ __forceinline__ static v4f mul(const Frag& a, const Frag& b, v4f c) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
-    return c;
+  static constexpr int SUB = 4;   // products of a step, one k each
+  __device__ __forceinline__ static v4f mul(const Frag& a, const Frag& b, v4f c, int r) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], b[r], c, 0, 0, 0);
   }
 };
 template <> struct Mfma<OT_BF16> {
   typedef v8bf Frag;         // eight k of one row: k = 8 (lane / 16) + 0..7 of 32
-  __device__ __forceinline__ static v4f mul(const Frag& a, const Frag& b, v4f c) {
+  static constexpr int SUB = 1;
+  __device__ __forceinline__ static v4f mul(const Frag& a, const Frag& b, v4f c, int) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
 };
 template <> struct Mfma<OT_F16> {
   typedef v8h Frag;
-  __device__ __forceinline__ static v4f mul(const Frag& a, const Frag& b, v4f c) {
+  static constexpr int SUB = 1;
+  __device__ __forceinline__ static v4f mul(const Frag& a, const Frag& b, v4f c, int) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
   }
 };
@@ -60,15 +60,10 @@ struct Operand {
   static_assert(MODE == KC || TYPE == OT_F32 || BX >= 64, "a row of four pairs at least");
   static_assert(BX % (8 * NW) == 0, "whole moves");
 
-  // A wave's moves are alike but for their rows: KC 8 NW apart; KR RSTEP apart, whose swizzle returns every 16 rows.
-  static constexpr int RSTEP = NW * 64 / RS;
-  static constexpr int OFFS = MODE == KC || RSTEP % 16 == 0 ? 1 : 2;
-  static_assert(MODE == KC || RSTEP % 8 == 0, "rows 8 or 16 apart");
-
   const char* base;
   int64_t step;        // bytes from a slice to the next
   uint32_t ldb;        // bytes from a row to the next
-  uint32_t off[OFFS];  // this lane's 16 bytes in the wave's first moves
+  uint32_t off[MOVES]; // this lane's 16 bytes in each of the wave's moves
   uint32_t kat, kdim;  // KC: the summed index that they hold, in their slice; its end
   uint32_t bytes;      // KC: of the rows that exist
   int wave;
@@ -80,26 +75,30 @@ struct Operand {
   // p: the tile's first row (KC: rows ld apart; KR: the first row of the summed index at the tile's first column);
   // xdim: rows that exist
   __device__ __forceinline__ void open(const void* p, int64_t ld, int xdim, int64_t kd, int w, int lane) {
-    base = (const char*)p;
+    // scalars, though they come from offsets that were read by a vector load
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)(uint64_t)p);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)p >> 32));
+    base = (const char*)(((uint64_t)hi << 32) | lo);
     wave = w;
-    kdim = (uint32_t)kd;
+    kdim = __builtin_amdgcn_readfirstlane((uint32_t)kd);
     ldb = (uint32_t)(ld * ES);
     step = MODE == KC ? 128 : (int64_t)KS * ldb;
+    kat = 0;
+    bytes = 0;
     if (MODE == KC) {
-      const int x = 8 * w + (lane >> 3), q = (lane & 7) ^ (x & 7);
+      bytes = __builtin_amdgcn_readfirstlane((uint32_t)min(xdim, BX) * ldb);
+      const int q = (lane & 7) ^ (lane >> 3);   // row % 8 is lane / 8
       kat = q * EV;
-      off[0] = (uint32_t)x * ldb + 16 * q;
-      bytes = (uint32_t)min(xdim, BX) * ldb;
+#pragma unroll
+      for (int j = 0; j < MOVES; ++j) off[j] = (uint32_t)(8 * (w + NW * j) + (lane >> 3)) * ldb + 16 * q;
     } else {
 #pragma unroll
-      for (int v = 0; v < OFFS; ++v) {
-        const int slot = (w + NW * v) * 64 + lane, row = slot / RS, s = slot % RS;
+      for (int j = 0; j < MOVES; ++j) {
+        const int slot = (w + NW * j) * 64 + lane, row = slot / RS, s = slot % RS;
         const int col = TYPE == OT_F32 ? 16 * ((s >> 2) ^ kr_swizzle(row)) + 4 * (s & 3)
                                        : 16 * ((s >> 1) ^ kr_swizzle(row)) + 8 * (s & 1);
-        off[v] = col < xdim ? (uint32_t)(row - v * RSTEP) * ldb + col * ES : pieces::kOob;
+        off[j] = col < xdim ? (uint32_t)row * ldb + col * ES : pieces::kOob;
       }
-      kat = 0;
-      bytes = 0;
     }
   }
 
@@ -112,15 +111,11 @@ struct Operand {
       const int64_t left = (int64_t)kdim - (int64_t)kt * KS;
       size = left <= 0 ? 0u : (uint32_t)min((int64_t)0x7FFFFFF0, left * ldb);
     }
-    const uint64_t v = (uint64_t)p;
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
-    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-    const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)(((uint64_t)hi << 32) | lo), (short)0,
-                                                        __builtin_amdgcn_readfirstlane(size), 0x00020000);
+    const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)p, (short)0, size, 0x00020000);
     const bool in = MODE == KR || (uint32_t)kt * KS + kat < kdim;
 #pragma unroll
     for (int j = 0; j < MOVES; ++j) {
-      const uint32_t o = (in ? off[j % OFFS] : pieces::kOob) + (uint32_t)(j * (MODE == KC ? 8 * NW : RSTEP)) * ldb;
+      const uint32_t o = in ? off[j] : pieces::kOob;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (pieces::lds_void*)(lds + (at + (wave + NW * j) * 1024)), 16, o, 0, 0, 0);
     }
   }
@@ -189,7 +184,6 @@ struct Tile {
   static constexpr int STAGE = P::BYTES + Q::BYTES;
   static constexpr int KS = P::KS;
   static constexpr int FETCHES = P::MOVES + Q::MOVES;
-  static constexpr int READS = (MP == KC ? IB : (TYPE == OT_F32 ? 4 : 2) * IB) + (MQ == KC ? JB : (TYPE == OT_F32 ? 4 : 2) * JB);
 
   // acc[i][j][r]: row 16 i + lane % 16, column 16 j + 4 (lane / 16) + r of the wave's part (Q feeds the matrix
   // instruction's rows, so that a lane holds four consecutive columns of C)
@@ -209,57 +203,71 @@ struct Tile {
       for (int j = 0; j < JB; ++j) acc[i][j] = (v4f){0.f, 0.f, 0.f, 0.f};
     const int nk = (int)((depth + 2 * KS - 1) / (2 * KS)) * 2;   // an even number of slices
     if (nk == 0) return;
-    auto fetch = [&](lds_t* stage, int kt) {
-      op.fetch(stage, 0, kt);
-      oq.fetch(stage, P::BYTES, kt);
-    };
-    fetch(lds0, 0);
-    fetch(lds1, 1);
+    fetch(lds0, op, oq, 0);
+    fetch(lds1, op, oq, 1);
     stage_barrier<FETCHES>();    // slice 0 has landed
     if (wm * IB * 16 >= rows || wn * JB * 16 >= cols) {
       // nothing of this wave's part is stored: it only moves its share, and leaves the matrix unit to the others
       for (int kt = 0; kt < nk; kt += 2) {
         stage_barrier<FETCHES>();
-        fetch(lds0, kt + 2);
+        fetch(lds0, op, oq, kt + 2);
         stage_barrier<FETCHES>();
         stage_barrier<FETCHES>();
-        fetch(lds1, kt + 3);
+        fetch(lds1, op, oq, kt + 3);
         stage_barrier<FETCHES>();
       }
       pieces::wait_loads();
       return;
     }
-    typename Mfma<TYPE>::Frag fp[2][IB], fq[2][JB];
+    // A part of whose blocks only the first half has rows multiplies those alone.
+    if (IB > 1 && rows - wm * IB * 16 <= IB * 8) slices<(IB + 1) / 2>(lds0, lds1, op, oq, nk, acc);
+    else slices<IB>(lds0, lds1, op, oq, nk, acc);
+    pieces::wait_loads();      // nothing may still move into this workgroup's LDS
+  }
+
+  __device__ __forceinline__ static void fetch(lds_t* stage, const P& op, const Q& oq, int kt) {
+    op.fetch(stage, 0, kt);
+    oq.fetch(stage, P::BYTES, kt);
+  }
+
+  // the wave's products over nk slices, of its first IA row blocks
+  template <int IA>
+  __device__ __forceinline__ static void slices(lds_t* lds0, lds_t* lds1, const P& op, const Q& oq, int nk,
+                                                v4f (&acc)[IB][JB]) {
+    typename Mfma<TYPE>::Frag fp[2][IA], fq[2][JB];
     auto read = [&](const lds_t* stage, int s) {
 #pragma unroll
       for (int j = 0; j < JB; ++j) fq[s][j] = oq.read(stage, P::BYTES, j, s);
 #pragma unroll
-      for (int i = 0; i < IB; ++i) fp[s][i] = op.read(stage, 0, i, s);
+      for (int i = 0; i < IA; ++i) fp[s][i] = op.read(stage, 0, i, s);
     };
     auto multiply = [&](int s, int i0, int i1) {
 #pragma unroll
-      for (int i = i0; i < i1; ++i)
+      for (int r = 0; r < Mfma<TYPE>::SUB; ++r)   // products of one block apart: each waits for the one before
 #pragma unroll
-        for (int j = 0; j < JB; ++j) acc[i][j] = Mfma<TYPE>::mul(fq[s][j], fp[s][i], acc[i][j]);
+        for (int i = i0; i < i1; ++i)
+#pragma unroll
+          for (int j = 0; j < JB; ++j) acc[i][j] = Mfma<TYPE>::mul(fq[s][j], fp[s][i], acc[i][j], r);
     };
     // A slice's first half is multiplied while its second is read; then everyone has read the stage, and the slice
     // two further on is fetched into it, which has a slice and a half to arrive; the second half is multiplied while
     // the next slice's first is read.  (With one barrier, fetches issued behind the first half: 0.7 slices to arrive,
     // and 41 % of the waves' time spent waiting.)  The last rounds fetch and read past the operands, zeros, so that a
     // round is one block of code.
-    constexpr int IH = (IB + 1) / 2;
+    constexpr int IH = (IA + 1) / 2;
+    constexpr int READS = (MP == KC ? IA : (TYPE == OT_F32 ? 4 : 2) * IA) + (MQ == KC ? JB : (TYPE == OT_F32 ? 4 : 2) * JB);
     auto round = [&](lds_t* now, const lds_t* next, int kt) {
       read(now, 1);
       multiply(0, 0, IH);
       interleave<READS, 0, IH * JB>();
       stage_barrier<FETCHES>();    // everyone has read the stage
-      fetch(now, kt + 2);
-      multiply(0, IH, IB);
-      interleave<0, FETCHES, (IB - IH) * JB>();
+      fetch(now, op, oq, kt + 2);
+      multiply(0, IH, IA);
+      interleave<0, FETCHES, (IA - IH) * JB>();
       stage_barrier<FETCHES>();    // slice kt + 1 has landed
       read(next, 0);
-      multiply(1, 0, IB);
-      interleave<READS, 0, IB * JB>();
+      multiply(1, 0, IA);
+      interleave<READS, 0, IA * JB>();
       __builtin_amdgcn_sched_barrier(0);
     };
     read(lds0, 0);
@@ -267,14 +275,13 @@ struct Tile {
       round(lds0, lds1, kt);
       round(lds1, lds0, kt + 1);
     }
-    pieces::wait_loads();      // nothing may still move into this workgroup's LDS
   }
 
   // spreads LDS reads and fetches between the products of a part of a round
   template <int NR, int NF, int BLOCKS>
   __device__ __forceinline__ static void interleave() {
-    constexpr int PRODUCTS = BLOCKS * (TYPE == OT_F32 ? 4 : 1);
-    constexpr int PER = PRODUCTS / (NR + NF) < 1 ? 1 : PRODUCTS / (NR + NF);
+    constexpr int PRODUCTS = BLOCKS * Mfma<TYPE>::SUB;
+    constexpr int PER = NR + NF == 0 || PRODUCTS / (NR + NF) < 1 ? 1 : PRODUCTS / (NR + NF);
 #pragma unroll
     for (int k = 0; k < NR; ++k) {
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);     // an LDS read

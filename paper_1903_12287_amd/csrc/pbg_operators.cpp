@@ -125,6 +125,16 @@ struct Operands {
   }
 };
 
+// the plan's tables and partial sums in the workspace from p (a multiple of 256 bytes) on
+void place_plan(GroupPlan* plan, char* p, int64_t m, int64_t k) {
+  plan->partial = (float*)p;
+  p += (size_t)plan->partial_slots * m * k * 4;
+  p = (char*)(((uintptr_t)p + 15) & ~(uintptr_t)15);
+  plan->rows.at = (int4*)p;
+  plan->da.at = plan->rows.at + plan->rows.count;
+  plan->join = (int2*)(plan->da.at + plan->da.count);
+}
+
 pbg_status check_group(pbg_ctx* ctx, int32_t dtype, const int64_t* offsets, int32_t groups, int64_t n, int32_t in_dim,
                        int32_t out_dim) {
   if (dtype < PBG_TYPE_F32 || dtype > PBG_TYPE_F16) return set_err(ctx, PBG_ERR_INVALID_ARG, "unknown type %d", dtype);
@@ -164,17 +174,19 @@ extern "C" pbg_status pbg_group_linear(pbg_ctx* ctx, int32_t dtype, const void* 
     ops.add(&g.x, &g.ldx, n, in_dim);
     ops.add(&g.a, &g.lda, (int64_t)groups * out_dim, in_dim);
   }
-  st = workspace(ctx, ops.bytes);
+  GroupPlan plan = plan_group(dtype, GP_FORWARD, n, groups, out_dim, in_dim, false);
+  st = workspace(ctx, ops.bytes + plan.bytes());
   if (st != PBG_OK) return st;
   ops.place((char*)ctx->ops_ws);
+  place_plan(&plan, (char*)ctx->ops_ws + ops.bytes, out_dim, in_dim);
   g.kd = ops.padded(in_dim);
   g.a_group = (int64_t)out_dim * g.lda;
   ctx->edge_dirty = true;
-  launch_check_offsets(offsets, groups, n, ctx->edge_flag, ctx->cs);
+  launch_group_plan(plan, offsets, groups, n, ctx->edge_flag, ctx->cs);
   launch_group_pack(dtype, ops.count, ops.src, ops.dst, ops.ld, ops.rows, ops.width, ops.wp, ctx->cs);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) {
-    if (!launch_group_product(g, dtype, GP_FORWARD, GroupPlan{}, ctx->cs)) {
+    if (!launch_group_product(g, dtype, GP_FORWARD, plan, ctx->cs)) {
       (void)hipStreamSynchronize(ctx->cs);
       return set_err(ctx, PBG_ERR_UNSUPPORTED, "more tiles than a launch holds");
     }
@@ -204,27 +216,27 @@ extern "C" pbg_status pbg_group_linear_backward(pbg_ctx* ctx, int32_t dtype, con
   for (const Rows* in : {&rx, &ra, &rdy, &ro})
     if (overlap(rdx, *in) || overlap(rda, *in)) return set_err(ctx, PBG_ERR_INVALID_ARG, "an output overlaps an input");
   if (overlap(rdx, rda)) return set_err(ctx, PBG_ERR_INVALID_ARG, "dx and da overlap");
+  if (!dx && !da) return PBG_OK;
   st = ensure_edge_flags(ctx);
   if (st != PBG_OK) return st;
   GroupArgs g{x, a, dy, nullptr, ldx, in_dim, lddy, 0, 0, offsets, groups, n, in_dim, out_dim, in_dim, out_dim,
               ctx->edge_flag, ctx->edge_hflag};
   Operands ops(dtype);
-  GroupPlan plan{};
+  GroupPlan plan = plan_group(dtype, dx ? GP_DX : GP_DA, n, groups, out_dim, in_dim, da != nullptr);
   if (n > 0) {
     ops.add(&g.dy, &g.lddy, n, out_dim);
     if (da) ops.add(&g.x, &g.ldx, n, in_dim);
     if (dx) ops.add(&g.a, &g.lda, gm, in_dim);
   }
-  if (da) plan_group_da(n, groups, out_dim, in_dim, &plan);
-  st = workspace(ctx, ops.bytes + (size_t)plan.partial_slots * out_dim * in_dim * 4);
+  st = workspace(ctx, ops.bytes + plan.bytes() + 16 + (size_t)plan.partial_slots * out_dim * in_dim * 4);
   if (st != PBG_OK) return st;
   ops.place((char*)ctx->ops_ws);
-  plan.partial = (float*)((char*)ctx->ops_ws + ops.bytes);
+  place_plan(&plan, (char*)ctx->ops_ws + ops.bytes, out_dim, in_dim);
   g.kd = ops.padded(in_dim);
   g.md = ops.padded(out_dim);
   g.a_group = (int64_t)out_dim * g.lda;
   ctx->edge_dirty = true;
-  launch_check_offsets(offsets, groups, n, ctx->edge_flag, ctx->cs);
+  launch_group_plan(plan, offsets, groups, n, ctx->edge_flag, ctx->cs);
   launch_group_pack(dtype, ops.count, ops.src, ops.dst, ops.ld, ops.rows, ops.width, ops.wp, ctx->cs);
   hipError_t e = hipGetLastError();
   bool fits = true;
