@@ -141,6 +141,8 @@ constexpr int kPackRows = 16;
 template <int TYPE>
 __global__ __launch_bounds__(256) void group_pack_kernel(PackArgs a) {
   typedef typename Elem<TYPE>::T T;
+  typedef typename Vec<TYPE>::V V;
+  constexpr int N = Vec<TYPE>::N;
   const int w = blockIdx.x >= a.first[2] ? 2 : (blockIdx.x >= a.first[1] ? 1 : 0);
   const int64_t r0 = (int64_t)(blockIdx.x - a.first[w]) * kPackRows;
   const int64_t r1 = min(a.rows[w], r0 + kPackRows);
@@ -148,7 +150,14 @@ __global__ __launch_bounds__(256) void group_pack_kernel(PackArgs a) {
   for (int64_t r = r0 + wave; r < r1; r += 4) {
     const T* s = (const T*)a.src[w] + r * a.ld[w];
     T* d = (T*)a.dst[w] + r * a.wp[w];
-    for (int c = lane; c < a.wp[w]; c += 64) d[c] = c < a.width[w] ? s[c] : (T)0.0f;
+    for (int c = lane * N; c < a.wp[w]; c += 64 * N) {   // wp is a multiple of N
+      if (c + N <= a.width[w]) {
+        *(V*)(d + c) = *(const V*)(s + c);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) d[c + j] = c + j < a.width[w] ? s[c + j] : (T)0.0f;
+      }
+    }
   }
 }
 
@@ -180,7 +189,9 @@ bool launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) 
   L.blocks = (uint32_t)blocks;
   group_da_kernel<TYPE, 128, 128, 2, 2><<<L.blocks, 256, 0, s>>>(g, L);
   if (p.partial_slots > 0) {
-    const dim3 grid((unsigned)std::min<int64_t>(tiles_of((int64_t)g.m * g.k, 64), 4096), (unsigned)p.partial_slots);
+    // most places hold no group's first sum, and their workgroups end at once: 16,384 in all
+    const int64_t chunks = std::max<int64_t>(64, 16384 / p.partial_slots);
+    const dim3 grid((unsigned)std::min(tiles_of((int64_t)g.m * g.k, 64), chunks), (unsigned)p.partial_slots);
     group_join_kernel<TYPE><<<grid, 256, 0, s>>>(g, L);
   }
   return true;
@@ -188,17 +199,17 @@ bool launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) 
 
 // Rows of a tile of y or dx, 2^shift, by the average group.  A tile as tall as its group reads the group's matrix once
 // and multiplies few rows that are not there; of 256 x 256 the forward product of 16 bits does a third more a second
-// than of 128 x 128, where there are tiles enough for the 256 compute units (dx, whose matrix is read through the
-// transposing LDS read, runs out of registers there).
+// than of 128 x 128 (dx, whose matrix is read through the transposing LDS read, runs out of registers there).  Large
+// tiles only where there are some for each of the 256 compute units.
 int row_shift(int type, int which, int64_t n, int groups, int64_t cols) {
   const int64_t average = n / groups;
-  if (type != OT_F32 && which == GP_FORWARD && average >= 256 && n / 256 * tiles_of(cols, 256) >= 256) return 8;
-  return average >= 64 ? 7 : 5;
+  if (type != OT_F32 && average >= 256 && n / 256 * tiles_of(cols, 256) >= 256) return 8;
+  return average >= 64 && n / 128 * tiles_of(cols, 128) >= 512 ? 7 : 5;
 }
 
 template <int TYPE, int WHICH>
 bool launch_rows_by_size(const GroupArgs& g, const GroupPlan& p, const Launch& L, hipStream_t s) {
-  if constexpr (TYPE != OT_F32 && WHICH == GP_FORWARD) {
+  if constexpr (TYPE != OT_F32) {
     if (p.rows.shift == 8) return launch_rows<TYPE, WHICH, 256, 256, 2, 4>(g, p, L, s);
   }
   if (p.rows.shift == 7) return launch_rows<TYPE, WHICH, 128, 128, 2, 2>(g, p, L, s);
@@ -301,9 +312,9 @@ GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int6
   // Rows of a slot of da: enough slots for a few workgroups on each of the 256 compute units, where the matrices' tiles
   // alone are not; with tiles enough, only groups of four times the average and more are cut.
   const int64_t tiles = tiles_of(m, 128) * tiles_of(k, 128);
-  int64_t rows = std::max<int64_t>(256, n * tiles / 1024);
+  int64_t rows = std::max<int64_t>(128, n * tiles / 1024);
   if (groups * tiles >= 512) rows = std::max(rows, 4 * n / groups);
-  int shift = 8;
+  int shift = 7;
   while (shift < 31 && ((int64_t)1 << shift) < rows) ++shift;
   // the partial sums stay below 512 MB, and a grid has 65,535 of them
   while (shift < 31 && (((2 * n) >> shift) * m * k * 4 > (512ll << 20) || (2 * n) >> shift > 65535)) ++shift;

@@ -108,8 +108,8 @@ struct Operand {
     const char* p = base + kt * step;
     uint32_t size = bytes;
     if (MODE == KR) {
-      const int64_t left = (int64_t)kdim - (int64_t)kt * KS;
-      size = left <= 0 ? 0u : (uint32_t)min((int64_t)0x7FFFFFF0, left * ldb);
+      const uint32_t done = (uint32_t)kt * KS;
+      size = __builtin_amdgcn_readfirstlane(min(max(kdim, done) - done, (uint32_t)KS) * ldb);
     }
     const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)p, (short)0, size, 0x00020000);
     const bool in = MODE == KR || (uint32_t)kt * KS + kat < kdim;
