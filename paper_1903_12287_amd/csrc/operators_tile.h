@@ -249,12 +249,12 @@ struct Tile {
 #pragma unroll
           for (int j = 0; j < JB; ++j) acc[i][j] = Mfma<TYPE>::mul(fq[s][j], fp[s][i], acc[i][j], r);
     };
-    // A slice's first half is multiplied while its second is read; then everyone has read the stage, and the slice
-    // two further on is fetched into it, which has a slice and a half to arrive; the second half is multiplied while
-    // the next slice's first is read.  (With one barrier, fetches issued behind the first half: 0.7 slices to arrive,
-    // and 41 % of the waves' time spent waiting.)  The last rounds fetch and read past the operands, zeros, so that a
-    // round is one block of code.
-    constexpr int IH = (IA + 1) / 2;
+    // A slice's second half is read behind the first products of its first; then everyone has read the stage, and the
+    // slice two further on is fetched into it, which has more than a slice and a half to arrive; the second half is
+    // multiplied while the next slice's first is read.  (With one barrier, fetches issued behind the first half: 0.7
+    // slices to arrive, and 41 % of the waves' time spent waiting.)  The last rounds fetch and read past the operands,
+    // zeros, so that a round is one block of code.
+    constexpr int IH = (IA + 3) / 4;
     constexpr int READS = (MP == KC ? IA : (TYPE == OT_F32 ? 4 : 2) * IA) + (MQ == KC ? JB : (TYPE == OT_F32 ? 4 : 2) * JB);
     auto round = [&](lds_t* now, const lds_t* next, int kt) {
       read(now, 1);
