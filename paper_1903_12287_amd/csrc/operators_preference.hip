@@ -123,12 +123,13 @@ __device__ __forceinline__ Stats join_waves(Stats a) {
   return a;
 }
 
-// a counted row's stats and log probability; a row without a distribution does not count
+// a counted row's stats and log probability; a row without a distribution does not count.  The logarithm is taken in
+// float64: rounded to float32, at a size of ten, it is what a sequence of many rows would be off by.
 __device__ __forceinline__ void finish_row(const Stats& a, float z_label, float2& stats, double& picked) {
   const bool none = a.m == -INFINITY && a.s == 0.0f;
-  const float ls = none ? 0.0f : logf(a.s);
-  stats = make_float2(a.m, ls);
-  picked = none ? 0.0 : (double)(z_label - a.m) - (double)ls;
+  const double ls = none ? 0.0 : log((double)a.s);
+  stats = make_float2(a.m, (float)ls);
+  picked = none ? 0.0 : ((double)z_label - (double)a.m) - ls;
 }
 
 // Many rows, whose labels and offsets have been checked: WAVE, a wave a row, else a workgroup.

@@ -39,6 +39,9 @@ pbg_status begin_call(pbg_ctx* ctx, const char* name) {
   if (!ctx) return PBG_ERR_INVALID_ARG;
   if (ctx->invalid) return set_err(ctx, PBG_ERR_STATE, "context failed to initialise");
   ctx->err.clear();
+  // an error that is pending in the runtime ends the call before it has launched anything
+  const hipError_t pending = hipGetLastError();
+  if (pending != hipSuccess) return set_err(ctx, PBG_ERR_DEVICE, "pending ahead of %s: %s", name, hipGetErrorString(pending));
   int cur = -1;
   if (hipGetDevice(&cur) != hipSuccess || cur != ctx->device)
     return set_err(ctx, PBG_ERR_STATE, "the context's device %d must be current (current: %d)", ctx->device, cur);

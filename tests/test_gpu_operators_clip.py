@@ -41,7 +41,7 @@ def check(got, g, factor):
     assert bool(((got.double().cpu() - want).abs() <= tol).all())
 
 
-SIZES = [[1], [5], [64, 1, 3], [4096], [16_384, 16_385, 16_383], [100_003, 7], [1] * 100, [1_000_003],
+SIZES = [[1], [5], [64, 1, 3], [4096], [16_384, 16_385, 16_383], [100_003, 7], [1] * 100, [1_000_003], [9_000_001, 3],
          [30_000] * 97 + [5, 70_001], list(range(1, 210, 7))]
 
 

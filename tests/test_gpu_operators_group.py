@@ -1,4 +1,6 @@
 """Products with one matrix per group of rows, and their gradients, against float64."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -104,6 +106,22 @@ def test_few_rows_in_many_groups(ctx, t):
 def test_wide_products(ctx, t, sizes, k, m):
     """Enough rows and columns for the largest tiles, forward, dx and da."""
     run_case(ctx, TYPES[t], sizes, k, m, seed=1)
+
+
+@pytest.mark.parametrize("t,small,large", [("f16", -20, 8), ("f16", -16, 8), ("bf16", -130, 20), ("f32", -140, 30)])
+def test_values_below_the_normal_range(ctx, t, small, large):
+    """One factor of a product below its type's normal range, the other large: the product keeps every bit."""
+    dt, n, k, m = TYPES[t], 40, 64, 48
+    rng = np.random.default_rng(0)
+    x, a = rows(rng, n, k, dt, scale=2.0 ** small), rows(rng, m, k, dt, scale=2.0 ** large).view(1, m, k)
+    dy = rows(rng, n, m, dt, scale=2.0 ** large)
+    off = torch.tensor([0, n], dtype=torch.int64, device="cuda")
+    y, da = torch.empty(n, m, dtype=dt, device="cuda"), torch.empty(1, m, k, dtype=dt, device="cuda")
+    ops.pbg_group_linear(ctx, x, a, off, y)
+    ops.pbg_group_linear_backward(ctx, x, None, off, dy, None, da)
+    exact, size = group_products(x, a, dy, [0, n])
+    check(("y", dt), y, exact["y"], size["y"], k)
+    check(("da", dt), da, exact["da"], size["da"], n)
 
 
 @pytest.mark.parametrize("t", TYPES)
@@ -273,6 +291,22 @@ def test_refusals(ctx):
                  (0, p[0] + 2, 4, p[1], p[2], 2, 10, 4, 6, p[3], 6), (0, p[0], 1 << 21, p[1], p[2], 2, 10, 4, 6, p[3], 6)):
         assert lib.pbg_group_linear(ctx, *args) == 1, args
     assert bool((y == SENTINEL).all())
+
+
+def test_neither_gradient_and_pending_errors(ctx):
+    x, a = torch.ones(4, 4, device="cuda"), torch.ones(1, 4, 4, device="cuda")
+    y = torch.full((4, 4), SENTINEL, device="cuda")
+    off = torch.tensor([0, 4], dtype=torch.int64, device="cuda")
+    ops.pbg_group_linear_backward(ctx, x, a, off, y, None, None)
+    bad = torch.tensor([0, 5], dtype=torch.int64, device="cuda")
+    ops.pbg_group_linear_backward(ctx, x, a, bad, y, None, None)   # nothing to write, nothing looked at
+    lib = ctypes.CDLL(pbg.LIB_PATH)   # and the HIP runtime it is linked against
+    assert lib.hipSetDevice(9999) != 0
+    with pytest.raises(pbg.PbgError, match="pending"):
+        ops.pbg_group_linear(ctx, x, a, off, y)
+    assert bool((y == SENTINEL).all())
+    ops.pbg_group_linear(ctx, x, a, off, y)
+    assert bool((y == 4).all())
 
 
 def test_a_capturing_stream_is_refused_and_its_capture_goes_on(ctx):

@@ -121,6 +121,13 @@ def test_sizes(ctx, t, lengths, V):
 
 
 @pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("V", [70, 2_501])
+def test_many_rows(ctx, t, V):
+    """More rows than are cut into segments, a wave or a workgroup each."""
+    compare(Case(TYPES[t], [1_500, 0, 900, 703], V, first=1, tail=2, hidden=0.1, seed=V), ctx)
+
+
+@pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("V,pad,front", [(200, 8, 0), (200, 1, 0), (200, 0, 1), (199, 3, 5), (4_097, 7, 2), (40_001, 1, 3)])
 def test_strides_and_alignments(ctx, t, V, pad, front):
     compare(Case(TYPES[t], [4, 0, 7, 3], V, first=2, tail=3, pad=pad, front=front, seed=pad), ctx)
