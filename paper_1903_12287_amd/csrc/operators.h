@@ -43,8 +43,9 @@ struct GroupPlan {
   GroupSlots da;           // da: a slot's rows are summed by one workgroup
   int64_t partial_slots;   // places of partial sums, m k floats each (0: no group is longer than a slot)
   float* partial;
-  int2* join;              // [partial_slots]: {group whose first sum this is or -1, number of sums}
-  size_t bytes() const { return (size_t)(rows.count + da.count) * 16 + (size_t)partial_slots * 8; }
+  int64_t joins;           // entries of the table of groups of several sums: by group or by place, whichever are fewer
+  int4* join;              // {group or -1, number of sums, place of the first}
+  size_t bytes() const { return (size_t)(rows.count + da.count + joins) * 16; }
 };
 
 // what the call needs (count 0: not wanted), for workspace and launches

@@ -20,9 +20,8 @@ struct Launch {
   int shift;                  // da: rows of a slot: 2^shift
   int row_tiles, col_tiles;   // da: tiles of one matrix; y, dx: slots of all groups, tiles of the columns
   uint32_t blocks;
-  bool vec;                   // rows of the output start at multiples of four values
   float* partial;             // da: partial sums of the groups of several slots
-  const int2* join;
+  const int4* join;
 };
 
 // Tiles in bands of BAND slots, column by column: the workgroups that an XCD runs at a time share the rows of a few
@@ -59,7 +58,7 @@ __global__ __launch_bounds__(64 * WM * WN) void group_rows_kernel(GroupArgs g, L
     Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.x + r0 * g.ldx * ES, g.ldx, rows, a + (int64_t)j0 * g.lda * ES, g.lda, g.m - j0, g.kd, acc);
   else
     Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.dy + r0 * g.lddy * ES, g.lddy, rows, a + (int64_t)j0 * ES, g.lda, g.kd - j0, g.m, acc);
-  Tl::template store<TYPE>(acc, (char*)g.out + (r0 * g.ldo + j0) * ES, g.ldo, rows, width - j0, L.vec);
+  Tl::template store<TYPE>(acc, (char*)g.out + (r0 * g.ldo + j0) * ES, g.ldo, rows, width - j0);
 }
 
 // da: one slot of a group's rows, one tile of its matrix.  A group of one slot is stored; the slots of a longer one
@@ -83,31 +82,41 @@ __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Lau
           g.ldx, g.kd - j0, depth, acc);
   const int rows = min(BM, g.m - i0), cols = g.k - j0;
   if (slot.w < 0) {
-    Tl::template store<TYPE>(acc, (char*)g.out + (((int64_t)grp * g.m + i0) * g.k + j0) * ES, g.k, rows, cols, L.vec);
+    Tl::template store<TYPE>(acc, (char*)g.out + (((int64_t)grp * g.m + i0) * g.k + j0) * ES, g.k, rows, cols);
   } else {
     float* p = L.partial + (int64_t)slot.w * g.m * g.k;
-    Tl::template store<OT_F32>(acc, p + (int64_t)i0 * g.k + j0, g.k, rows, cols, (g.k & 3) == 0);
+    Tl::template store<OT_F32>(acc, p + (int64_t)i0 * g.k + j0, g.k, rows, cols);
   }
 }
 
-// Adds a group's partial sums: 64 elements a workgroup, each of its four waves a quarter of the slots in their order,
-// then the waves in theirs.  (One thread an element over all slots: 65 us for 78 slots of 100 x 100, loads one behind
+// Adds a group's partial sums: of more than eight, 64 elements a workgroup, each of its four waves a quarter of the slots
+// in their order, then the waves in theirs.  (One thread an element over all slots: 65 us for 78 slots of 100 x 100, loads one behind
 // the other.)
 template <int TYPE>
 __global__ __launch_bounds__(256) void group_join_kernel(GroupArgs g, Launch L) {
   typedef typename Elem<TYPE>::T T;
   __shared__ float sums[4][64];
   if (!args_good(g.bad, g.host_bad)) return;
-  const int64_t slot = blockIdx.y;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int2 at = L.join[slot];
+  const int4 at = L.join[blockIdx.y];
   if (at.x < 0) return;
-  const int64_t grp = at.x;
+  const int64_t grp = at.x, place = at.z;
   const int parts = at.y;
   const int per = (parts + 3) >> 2, i0 = w * per, i1 = min(parts, i0 + per);
   const int64_t mk = (int64_t)g.m * g.k;
-  const float* p = L.partial + slot * mk;
+  const float* p = L.partial + place * mk;
   T* out = (T*)g.out + grp * mk;
+  if (parts <= 8) {   // few enough for one thread's loads
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < mk; e += (int64_t)gridDim.x * 256) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = u < parts ? p[u * mk + e] : 0.0f;
+#pragma unroll
+      for (int u = 1; u < 8; ++u) v[0] += v[u];
+      out[e] = (T)v[0];
+    }
+    return;
+  }
   for (int64_t e0 = (int64_t)blockIdx.x * 64; e0 < mk; e0 += (int64_t)gridDim.x * 64) {
     const int64_t e = min(e0 + lane, mk - 1);
     float s = 0.0f;
@@ -176,35 +185,45 @@ bool launch_rows(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s
   return true;
 }
 
-template <int TYPE>
+template <int TYPE, int B>
 bool launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) {
   L.slots = p.da.at;
   L.shift = p.da.shift;
   L.partial = p.partial;
   L.join = p.join;
-  L.row_tiles = (int)tiles_of(g.m, 128);
-  L.col_tiles = (int)tiles_of(g.k, 128);
+  L.row_tiles = (int)tiles_of(g.m, B);
+  L.col_tiles = (int)tiles_of(g.k, B);
   const int64_t blocks = p.da.count * L.row_tiles * L.col_tiles;
   if (blocks * 256 >= 1ll << 32) return false;
   L.blocks = (uint32_t)blocks;
-  group_da_kernel<TYPE, 128, 128, 2, 2><<<L.blocks, 256, 0, s>>>(g, L);
-  if (p.partial_slots > 0) {
-    // most places hold no group's first sum, and their workgroups end at once: 16,384 in all
-    const int64_t chunks = std::max<int64_t>(64, 16384 / p.partial_slots);
-    const dim3 grid((unsigned)std::min(tiles_of((int64_t)g.m * g.k, 64), chunks), (unsigned)p.partial_slots);
+  group_da_kernel<TYPE, B, B, 2, 2><<<L.blocks, 256, 0, s>>>(g, L);
+  if (p.joins > 0) {
+    // most entries are groups of one slot, whose workgroups end at once: 16,384 in all
+    const int64_t chunks = std::max<int64_t>(64, 16384 / p.joins);
+    const dim3 grid((unsigned)std::min(tiles_of((int64_t)g.m * g.k, 64), chunks), (unsigned)p.joins);
     group_join_kernel<TYPE><<<grid, 256, 0, s>>>(g, L);
   }
   return true;
 }
 
-// Rows of a tile of y or dx, 2^shift, by the average group.  A tile as tall as its group reads the group's matrix once
-// and multiplies few rows that are not there; of 256 x 256 the forward product of 16 bits does a third more a second
-// than of 128 x 128 (dx, whose matrix is read through the transposing LDS read, runs out of registers there).  Large
-// tiles only where there are some for each of the 256 compute units.
-int row_shift(int type, int which, int64_t n, int groups, int64_t cols) {
-  const int64_t average = n / groups;
-  if (type != OT_F32 && average >= 256 && n / 256 * tiles_of(cols, 256) >= 256) return 8;
-  return average >= 64 && n / 128 * tiles_of(cols, 128) >= 512 ? 7 : 5;
+// Rows and columns of a tile of da: in float32 the matrix unit sets the time, and more, smaller workgroups keep it busier
+// (8 groups, 40,000 rows, 100 x 100: both gradients 70 us for 75); in 16 bits reading the operands does (32 groups,
+// 16,384 rows, 2,048 x 2,048: 524 us for 448).
+constexpr int da_tile(int type) { return type == OT_F32 ? 64 : 128; }
+
+// Rows of a tile of y or dx, 2^shift, by the average group and the number of tiles.  Measured (us, 32 x 64 / 128 x 128 /
+// 256 x 256 tiles):
+//   float32, 256 groups of 32 rows of 400 x 400: 77 / 94; of 1,024 rows: 814 / 893; 8 groups of 2,048 of 4,096 x 4,096:
+//     4,657 / 4,018.  The matrix unit sets the time, and many small workgroups keep it busiest until operands are
+//     read over and over.
+//   bfloat16, 32 groups of 16 rows of 1,024 x 1,024: 29 / 34; of 32: 35 / 34; one of 1,024 rows of 512: 22 / 26 (16
+//     tiles); 4 groups of 128 rows of 2,048 x 2,048: 44 / 36 / 49; 32 of 512 rows: 569 / 194 / 191; 32 of 1,024 rows of
+//     2,048 x 4,096: 2,292 / 646 / 560; one of 8,192: 590 / 152 / 163 (2 tiles of 256 a compute unit).
+int row_shift(int type, int64_t n, int groups, int64_t cols) {
+  const int64_t average = n / groups, tiles = n / 128 * tiles_of(cols, 128), wide = n / 256 * tiles_of(cols, 256);
+  if (type == OT_F32) return average >= 1024 && tiles >= 1024 ? 7 : 5;
+  if (average >= 256 && wide >= 1024) return 8;
+  return average >= 32 && tiles >= 64 ? 7 : 5;
 }
 
 template <int TYPE, int WHICH>
@@ -213,14 +232,13 @@ bool launch_rows_by_size(const GroupArgs& g, const GroupPlan& p, const Launch& L
     if (p.rows.shift == 8) return launch_rows<TYPE, WHICH, 256, 256, 2, 4>(g, p, L, s);
   }
   if (p.rows.shift == 7) return launch_rows<TYPE, WHICH, 128, 128, 2, 2>(g, p, L, s);
-  return launch_rows<TYPE, WHICH, 32, 128, 1, 4>(g, p, L, s);
+  return launch_rows<TYPE, WHICH, 32, 64, 1, 4>(g, p, L, s);
 }
 
 template <int TYPE>
 bool launch_typed(const GroupArgs& g, int which, const GroupPlan& p, hipStream_t s) {
   Launch L{};
-  L.vec = g.ldo % 4 == 0 && ((uintptr_t)g.out & (TYPE == OT_F32 ? 15 : 7)) == 0;
-  if (which == GP_DA) return launch_da<TYPE>(g, p, L, s);
+  if (which == GP_DA) return launch_da<TYPE, da_tile(TYPE)>(g, p, L, s);
   if (which == GP_FORWARD) return launch_rows_by_size<TYPE, GP_FORWARD>(g, p, L, s);
   return launch_rows_by_size<TYPE, GP_DX>(g, p, L, s);
 }
@@ -261,7 +279,7 @@ __device__ __forceinline__ int4 slot_of(const int64_t* offsets, int groups, int 
 // Offsets that are not in order are found here; what the tables then hold is not used.
 __global__ __launch_bounds__(256) void group_plan_kernel(GroupPlan p, const int64_t* offsets, int groups, int64_t n,
                                                          uint32_t* flag) {
-  const int64_t total = p.rows.count + p.da.count + p.partial_slots;
+  const int64_t total = p.rows.count + p.da.count + p.joins;
   const int64_t step = (int64_t)gridDim.x * 256;
   bool bad = false;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total || i <= groups; i += step) {
@@ -280,14 +298,16 @@ __global__ __launch_bounds__(256) void group_plan_kernel(GroupPlan p, const int6
       continue;
     }
     v -= p.da.count;
-    if (v < p.partial_slots) {
-      // a group of several slots holds two places at least, so at its first one it is the last group that starts there
-      // or before
-      const int g = group_at<true>(offsets, groups, p.da.shift, v);
-      int2 at = make_int2(-1, 0);
-      if (g >= 0 && first_place(offsets[g], p.da.shift) == v) {
-        const int64_t rows = offsets[g + 1] - offsets[g];
-        if (rows > (int64_t)1 << p.da.shift) at = make_int2(g, (int)((rows + ((int64_t)1 << p.da.shift) - 1) >> p.da.shift));
+    if (v < p.joins) {
+      // by group; or by place: a group of several slots holds two places at least, so at its first one it is the last
+      // group that starts there or before
+      const bool by_group = p.joins == groups;
+      const int g = by_group ? (int)v : group_at<true>(offsets, groups, p.da.shift, v);
+      int4 at = make_int4(-1, 0, 0, 0);
+      if (g >= 0) {
+        const int64_t place = first_place(offsets[g], p.da.shift), rows = offsets[g + 1] - offsets[g];
+        if (rows > (int64_t)1 << p.da.shift && (by_group || place == v))
+          at = make_int4(g, (int)((rows + ((int64_t)1 << p.da.shift) - 1) >> p.da.shift), (int)place, 0);
       }
       p.join[v] = at;
     }
@@ -298,20 +318,20 @@ __global__ __launch_bounds__(256) void group_plan_kernel(GroupPlan p, const int6
 }  // namespace
 
 void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, int64_t n, uint32_t* flag, hipStream_t s) {
-  const int64_t work = std::max<int64_t>(p.rows.count + p.da.count + p.partial_slots, groups + 1);
+  const int64_t work = std::max<int64_t>(p.rows.count + p.da.count + p.joins, groups + 1);
   group_plan_kernel<<<(unsigned)std::min<int64_t>(tiles_of(work, 256), 65536), 256, 0, s>>>(p, offsets, groups, n, flag);
 }
 
 GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int64_t k, bool want_da) {
   GroupPlan p{};
   if (which != GP_DA) {
-    p.rows.shift = row_shift(type, which, n, groups, which == GP_FORWARD ? m : k);
+    p.rows.shift = row_shift(type, n, groups, which == GP_FORWARD ? m : k);
     p.rows.count = (n >> p.rows.shift) + groups;
   }
   if (!want_da) return p;
   // Rows of a slot of da: enough slots for a few workgroups on each of the 256 compute units, where the matrices' tiles
   // alone are not; with tiles enough, only groups of four times the average and more are cut.
-  const int64_t tiles = tiles_of(m, 128) * tiles_of(k, 128);
+  const int64_t tiles = tiles_of(m, da_tile(type)) * tiles_of(k, da_tile(type));
   int64_t rows = std::max<int64_t>(128, n * tiles / 1024);
   if (groups * tiles >= 512) rows = std::max(rows, 4 * n / groups);
   int shift = 7;
@@ -321,6 +341,7 @@ GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int6
   p.da.shift = shift;
   p.da.count = (n >> shift) + groups;
   p.partial_slots = n > (int64_t)1 << shift ? (2 * n) >> shift : 0;
+  p.joins = std::min<int64_t>(groups, p.partial_slots);
   return p;
 }
 

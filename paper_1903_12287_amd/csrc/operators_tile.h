@@ -294,11 +294,11 @@ struct Tile {
     }
   }
 
-  // rounds the tile to TO and stores it; vec: rows of C start at multiples of four values' bytes
+  // rounds the tile to TO and stores it, four values at a time wherever a row starts
   template <int TO>
-  __device__ __forceinline__ static void store(const v4f (&acc)[IB][JB], void* c, int64_t ldc, int rows, int cols, bool vec) {
+  __device__ __forceinline__ static void store(const v4f (&acc)[IB][JB], void* c, int64_t ldc, int rows, int cols) {
     typedef typename Elem<TO>::T T;
-    typedef T T4 __attribute__((ext_vector_type(4)));
+    typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r0 = (w / WN) * IB * 16 + (lane & 15), c0 = (w % WN) * JB * 16 + 4 * (lane >> 4);
 #pragma unroll
@@ -310,7 +310,7 @@ struct Tile {
       for (int j = 0; j < JB; ++j) {
         const int col = c0 + 16 * j;
         const v4f v = acc[i][j];
-        if (vec && col + 3 < cols) {
+        if (col + 3 < cols) {
           *(T4*)(out + col) = (T4){(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
         } else {
 #pragma unroll

@@ -135,7 +135,7 @@ void place_plan(GroupPlan* plan, char* p, int64_t m, int64_t k) {
   p = (char*)(((uintptr_t)p + 15) & ~(uintptr_t)15);
   plan->rows.at = (int4*)p;
   plan->da.at = plan->rows.at + plan->rows.count;
-  plan->join = (int2*)(plan->da.at + plan->da.count);
+  plan->join = plan->da.at + plan->da.count;
 }
 
 pbg_status check_group(pbg_ctx* ctx, int32_t dtype, const int64_t* offsets, int32_t groups, int64_t n, int32_t in_dim,
