@@ -89,7 +89,7 @@ __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Lau
   }
 }
 
-// Adds a group's partial sums: of more than eight, 64 elements a workgroup, each of its four waves a quarter of the slots
+// Adds a group's partial sums: of more than 32, 64 elements a workgroup, each of its four waves a quarter of the slots
 // in their order, then the waves in theirs.  (One thread an element over all slots: 65 us for 78 slots of 100 x 100, loads one behind
 // the other.)
 template <int TYPE>
@@ -106,14 +106,17 @@ __global__ __launch_bounds__(256) void group_join_kernel(GroupArgs g, Launch L) 
   const int64_t mk = (int64_t)g.m * g.k;
   const float* p = L.partial + place * mk;
   T* out = (T*)g.out + grp * mk;
-  if (parts <= 8) {   // few enough for one thread's loads
+  if (parts <= 32) {   // few enough for one thread's loads, eight at a time
     for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < mk; e += (int64_t)gridDim.x * 256) {
-      float v[8];
+      float sum = p[e];
+      for (int i = 1; i < parts; i += 8) {
+        float v[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = u < parts ? p[u * mk + e] : 0.0f;
+        for (int u = 0; u < 8; ++u) v[u] = p[min(i + u, parts - 1) * mk + e];
 #pragma unroll
-      for (int u = 1; u < 8; ++u) v[0] += v[u];
-      out[e] = (T)v[0];
+        for (int u = 0; u < 8; ++u) sum += i + u < parts ? v[u] : 0.0f;
+      }
+      out[e] = (T)sum;
     }
     return;
   }
