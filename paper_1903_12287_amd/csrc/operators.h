@@ -39,18 +39,20 @@ struct GroupSlots {
 };
 
 struct GroupPlan {
+  bool tables;             // the tables below are written ahead of the products (else their pointers are NULL)
   GroupSlots rows;         // y, dx: a slot's rows are a tile's
   GroupSlots da;           // da: a slot's rows are summed by one workgroup
   int64_t partial_slots;   // places of partial sums, m k floats each (0: no group is longer than a slot)
   float* partial;
   int64_t joins;           // entries of the table of groups of several sums: by group or by place, whichever are fewer
   int4* join;              // {group or -1, number of sums, place of the first}
-  size_t bytes() const { return (size_t)(rows.count + da.count + joins) * 16; }
+  size_t bytes() const { return tables ? (size_t)(rows.count + da.count + joins) * 16 : 0; }
 };
 
 // what the call needs (count 0: not wanted), for workspace and launches
 GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int64_t k, bool want_da);
-// the tables of slots, and offsets[0..groups] nondecreasing and within [0, n], else OPS_BAD_OFFSETS into *flag
+// the tables of slots, and offsets[0..groups] nondecreasing and within [0, n], else OPS_BAD_OFFSETS into *flag (nothing
+// where there are no tables)
 void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, int64_t n, uint32_t* flag, hipStream_t s);
 // up to three operands into rows of wp values, a multiple of 16 bytes, zeros behind `width`
 void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,

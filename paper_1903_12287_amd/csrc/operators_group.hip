@@ -5,7 +5,8 @@
 // The host does not know the groups' sizes, so it launches a workgroup for every slot of rows that there could be, and
 // a kernel ahead of the products (which also checks the offsets) writes down which group and rows a slot is.  (Every
 // workgroup searching the offsets itself: four loads one behind the other before its first fetch, 2.5 of the 10 us of
-// a workgroup with 32 rows of 400.)
+// a workgroup with 32 rows of 400.)  Offsets of up to 63 groups fit the lanes of a wave: there every wave reads and
+// checks them all in one load, and small products need no kernel ahead of them.
 #include <algorithm>
 
 #include "operators_tile.h"
@@ -16,13 +17,78 @@ using tile::KC;
 using tile::KR;
 
 struct Launch {
-  const int4* slots;
-  int shift;                  // da: rows of a slot: 2^shift
+  const int4* slots;          // NULL: up to 63 groups, every wave finds its slot itself
+  int shift;                  // rows of a slot: 2^shift
   int row_tiles, col_tiles;   // da: tiles of one matrix; y, dx: slots of all groups, tiles of the columns
   uint32_t blocks;
   float* partial;             // da: partial sums of the groups of several slots
   const int4* join;
 };
+
+// Rows cut into slots of 2^shift that never straddle two groups: group g's slots start at
+// floor(offsets[g] / 2^shift) + g.  A group of L rows needs ceil(L / 2^shift) of them and has
+// floor(end / 2^shift) - floor(start / 2^shift) + 1, which is never less; n / 2^shift + groups slots hold every group.
+// A group's places for partial sums start at floor(2 offsets[g] / 2^shift): one of L > 2^shift rows has at least
+// ceil(L / 2^shift) of them, so that 2 n / 2^shift places are enough, however many groups there are.
+__device__ __forceinline__ int64_t first_slot(int64_t offset, int g, int shift) { return (offset >> shift) + g; }
+__device__ __forceinline__ int64_t first_place(int64_t offset, int shift) { return (2 * offset) >> shift; }
+
+
+// slot v of slots of 2^shift rows, where group g holds rows [first, last) and slot v is at or behind its first slot
+__device__ __forceinline__ int4 slot_in(int g, int64_t first, int64_t last, int shift, int64_t v, bool places) {
+  const int64_t part = v - first_slot(first, g, shift), r0 = first + (part << shift);
+  if (part > 0 && r0 >= last) return make_int4(0, 0, -1, -1);
+  const int64_t rows = min((int64_t)1 << shift, last - r0);
+  const bool several = places && last - first > (int64_t)1 << shift;
+  return make_int4((int)r0, (int)rows, g, several ? (int)(first_place(first, shift) + part) : -1);
+}
+
+// the entry for a group's partial sums: {group or -1, number of sums, place of the first}
+__device__ __forceinline__ int4 join_of(int g, int64_t first, int64_t last, int shift) {
+  const int64_t rows = last - first;
+  if (rows <= (int64_t)1 << shift) return make_int4(-1, 0, 0, 0);
+  return make_int4(g, (int)((rows + ((int64_t)1 << shift) - 1) >> shift), (int)first_place(first, shift), 0);
+}
+
+// All offsets of up to 63 groups, one a lane.
+struct FewGroups {
+  int64_t mine;
+  int lane, groups;
+
+  // false: the offsets are not in order, which the first workgroup tells the host
+  __device__ __forceinline__ bool load(const GroupArgs& g) {
+    lane = threadIdx.x & 63;
+    groups = g.groups;
+    mine = g.offsets[min(lane, groups)];
+    const int64_t next = __shfl(mine, min(lane + 1, 63), 64);
+    const bool bad = mine < 0 || mine > g.n || next < mine;   // lanes past the last offset repeat it
+    if (__ballot(bad) == 0) return true;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *(volatile uint32_t*)g.host_bad = OPS_BAD_OFFSETS;
+    return false;
+  }
+  __device__ __forceinline__ int4 slot(int shift, int64_t v, bool places) const {
+    const int g = __popcll(__ballot(lane < groups && first_slot(mine, lane, shift) <= v)) - 1;
+    if (g < 0) return make_int4(0, 0, -1, -1);
+    return slot_in(g, __shfl(mine, g, 64), __shfl(mine, g + 1, 64), shift, v, places);
+  }
+  __device__ __forceinline__ int4 join(int shift, int g) const {
+    return join_of(g, __shfl(mine, g, 64), __shfl(mine, g + 1, 64), shift);
+  }
+};
+
+// slot v of the launch; false: the arguments are not good
+__device__ __forceinline__ bool find_slot(const GroupArgs& g, const Launch& L, int64_t v, bool places, int4& slot) {
+  if (L.slots) {
+    slot = L.slots[v];
+    return args_good(g.bad, g.host_bad);
+  }
+  FewGroups f;
+  if (!f.load(g)) return false;
+  const int4 at = f.slot(L.shift, v, places);
+  slot = make_int4(__builtin_amdgcn_readfirstlane(at.x), __builtin_amdgcn_readfirstlane(at.y),
+                   __builtin_amdgcn_readfirstlane(at.z), __builtin_amdgcn_readfirstlane(at.w));
+  return true;
+}
 
 // Tiles in bands of BAND slots, column by column: the workgroups that an XCD runs at a time share the rows of a few
 // slots and the matrix rows of a few columns, which its L2 then fetches once.
@@ -46,8 +112,8 @@ __global__ __launch_bounds__(64 * WM * WN) void group_rows_kernel(GroupArgs g, L
   uint32_t slot, col;
   band_tile<BAND>(at, L.row_tiles, L.col_tiles, slot, col);
   const int j0 = (int)col * BN;
-  const int4 at_slot = L.slots[slot];
-  if (!args_good(g.bad, g.host_bad)) return;
+  int4 at_slot;
+  if (!find_slot(g, L, slot, false, at_slot)) return;
   const int64_t r0 = at_slot.x;
   const int rows = at_slot.y, grp = at_slot.z;
   if (rows <= 0) return;
@@ -70,10 +136,10 @@ __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Lau
   __shared__ __attribute__((aligned(1024))) char lds0[Tl::STAGE], lds1[Tl::STAGE];
   const uint32_t at = tile::xcd_place(blockIdx.x, L.blocks);
   const int tiles = L.row_tiles * L.col_tiles;
-  const int4 slot = L.slots[at / tiles];
+  int4 slot;
+  if (!find_slot(g, L, at / tiles, true, slot)) return;
   const int t = (int)(at % tiles);
   const int i0 = t / L.col_tiles * BM, j0 = t % L.col_tiles * BN;
-  if (!args_good(g.bad, g.host_bad)) return;
   if (slot.z < 0) return;   // the first slot of an empty group stores zeros
   const int64_t r0 = slot.x, depth = slot.y;
   const int grp = slot.z;
@@ -96,9 +162,16 @@ template <int TYPE>
 __global__ __launch_bounds__(256) void group_join_kernel(GroupArgs g, Launch L) {
   typedef typename Elem<TYPE>::T T;
   __shared__ float sums[4][64];
-  if (!args_good(g.bad, g.host_bad)) return;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int4 at = L.join[blockIdx.y];
+  int4 at;
+  if (L.slots) {
+    if (!args_good(g.bad, g.host_bad)) return;
+    at = L.join[blockIdx.y];
+  } else {
+    FewGroups f;
+    if (!f.load(g)) return;
+    at = f.join(L.shift, blockIdx.y);
+  }
   if (at.x < 0) return;
   const int64_t grp = at.x, place = at.z;
   const int parts = at.y;
@@ -179,6 +252,7 @@ int64_t tiles_of(int64_t v, int b) { return (v + b - 1) / b; }
 template <int TYPE, int WHICH, int BM, int BN, int WM, int WN>
 bool launch_rows(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) {
   L.slots = p.rows.at;
+  L.shift = p.rows.shift;
   L.row_tiles = (int)p.rows.count;
   L.col_tiles = (int)tiles_of(WHICH == GP_FORWARD ? g.m : g.k, BN);
   const int64_t blocks = p.rows.count * L.col_tiles;
@@ -247,14 +321,6 @@ bool launch_typed(const GroupArgs& g, int which, const GroupPlan& p, hipStream_t
 }
 
 // ---- the tables of slots ---------------------------------------------------------------------------
-// Rows cut into slots of 2^shift that never straddle two groups: group g's slots start at
-// floor(offsets[g] / 2^shift) + g.  A group of L rows needs ceil(L / 2^shift) of them and has
-// floor(end / 2^shift) - floor(start / 2^shift) + 1, which is never less; n / 2^shift + groups slots hold every group.
-// A group's places for partial sums start at floor(2 offsets[g] / 2^shift): one of L > 2^shift rows has at least
-// ceil(L / 2^shift) of them, so that 2 n / 2^shift places are enough, however many groups there are.
-__device__ __forceinline__ int64_t first_slot(int64_t offset, int g, int shift) { return (offset >> shift) + g; }
-__device__ __forceinline__ int64_t first_place(int64_t offset, int shift) { return (2 * offset) >> shift; }
-
 // the last group whose first slot (PLACE: first place) is at most v, or -1
 template <bool PLACE>
 __device__ __forceinline__ int group_at(const int64_t* offsets, int groups, int shift, int64_t v) {
@@ -271,12 +337,7 @@ __device__ __forceinline__ int group_at(const int64_t* offsets, int groups, int 
 __device__ __forceinline__ int4 slot_of(const int64_t* offsets, int groups, int shift, int64_t v, bool places) {
   const int g = group_at<false>(offsets, groups, shift, v);
   if (g < 0) return make_int4(0, 0, -1, -1);
-  const int64_t first = offsets[g], last = offsets[g + 1];
-  const int64_t part = v - first_slot(first, g, shift), r0 = first + (part << shift);
-  if (part > 0 && r0 >= last) return make_int4(0, 0, -1, -1);
-  const int64_t rows = min((int64_t)1 << shift, last - r0);
-  const bool several = places && last - first > (int64_t)1 << shift;
-  return make_int4((int)r0, (int)rows, g, several ? (int)(first_place(first, shift) + part) : -1);
+  return slot_in(g, offsets[g], offsets[g + 1], shift, v, places);
 }
 
 // Offsets that are not in order are found here; what the tables then hold is not used.
@@ -307,11 +368,8 @@ __global__ __launch_bounds__(256) void group_plan_kernel(GroupPlan p, const int6
       const bool by_group = p.joins == groups;
       const int g = by_group ? (int)v : group_at<true>(offsets, groups, p.da.shift, v);
       int4 at = make_int4(-1, 0, 0, 0);
-      if (g >= 0) {
-        const int64_t place = first_place(offsets[g], p.da.shift), rows = offsets[g + 1] - offsets[g];
-        if (rows > (int64_t)1 << p.da.shift && (by_group || place == v))
-          at = make_int4(g, (int)((rows + ((int64_t)1 << p.da.shift) - 1) >> p.da.shift), (int)place, 0);
-      }
+      if (g >= 0 && (by_group || first_place(offsets[g], p.da.shift) == v))
+        at = join_of(g, offsets[g], offsets[g + 1], p.da.shift);
       p.join[v] = at;
     }
   }
@@ -321,12 +379,16 @@ __global__ __launch_bounds__(256) void group_plan_kernel(GroupPlan p, const int6
 }  // namespace
 
 void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, int64_t n, uint32_t* flag, hipStream_t s) {
+  if (!p.tables) return;
   const int64_t work = std::max<int64_t>(p.rows.count + p.da.count + p.joins, groups + 1);
   group_plan_kernel<<<(unsigned)std::min<int64_t>(tiles_of(work, 256), 65536), 256, 0, s>>>(p, offsets, groups, n, flag);
 }
 
 GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int64_t k, bool want_da) {
   GroupPlan p{};
+  // Tables written ahead cost a launch (2.5 us), offsets read by every workgroup 0.5 us for each workgroup that follows
+  // another on its compute unit: 2 of 38 us saved for 24 float16 rows of 2,048, 7 of 443 lost for 16,384 bfloat16 rows.
+  p.tables = groups > 63 || n * std::max(m, k) > 1 << 24;
   if (which != GP_DA) {
     p.rows.shift = row_shift(type, n, groups, which == GP_FORWARD ? m : k);
     p.rows.count = (n >> p.rows.shift) + groups;
@@ -344,7 +406,7 @@ GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int6
   p.da.shift = shift;
   p.da.count = (n >> shift) + groups;
   p.partial_slots = n > (int64_t)1 << shift ? (2 * n) >> shift : 0;
-  p.joins = std::min<int64_t>(groups, p.partial_slots);
+  p.joins = p.tables ? std::min<int64_t>(groups, p.partial_slots) : (p.partial_slots > 0 ? groups : 0);
   return p;
 }
 

@@ -305,9 +305,35 @@ __device__ __forceinline__ void row_gradient(const PrefArgs& p, int64_t t, int p
   }
 }
 
-template <int TYPE, bool WAVE>
+// what is not in order of the call's offsets and labels, by thread i0 of `step`: offsets nondecreasing within [0, n];
+// labels of rows inside a sequence below V (negative ones do not count)
+__device__ __forceinline__ uint32_t bad_args(const PrefArgs& p, int64_t i0, int64_t step) {
+  const int sequences = 2 * p.pairs;
+  const int64_t first = p.offsets[0], last = p.offsets[sequences];
+  uint32_t bad = 0;
+  for (int64_t i = i0; i <= sequences; i += step) {
+    const int64_t v = p.offsets[i];
+    if (v < 0 || v > p.n || (i < sequences && p.offsets[i + 1] < v)) bad |= OPS_BAD_OFFSETS;
+  }
+  for (int64_t t = i0; t < p.n; t += step)
+    if (t >= first && t < last && p.labels[t] >= p.V) bad |= OPS_BAD_LABEL;
+  return bad;
+}
+
+// CHECK: every workgroup checks the call's labels and offsets itself
+template <int TYPE, bool WAVE, bool CHECK>
 __global__ __launch_bounds__(256) void preference_backward_kernel(PrefArgs p) {
-  if (!args_good(p.bad, p.host_bad)) return;
+  if (CHECK) {
+    const uint32_t bad = bad_args(p, threadIdx.x, 256);
+    const int offsets = __syncthreads_or(bad & OPS_BAD_OFFSETS), labels = __syncthreads_or(bad & OPS_BAD_LABEL);
+    if (offsets || labels) {
+      if (blockIdx.x == 0 && threadIdx.x == 0)
+        *(volatile uint32_t*)p.host_bad = (offsets ? OPS_BAD_OFFSETS : 0u) | (labels ? OPS_BAD_LABEL : 0u);
+      return;
+    }
+  } else {
+    if (!args_good(p.bad, p.host_bad)) return;
+  }
   if (WAVE) {
     const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t < p.n) row_gradient<TYPE, 64>(p, t, 0, threadIdx.x & 63);
@@ -317,18 +343,8 @@ __global__ __launch_bounds__(256) void preference_backward_kernel(PrefArgs p) {
   }
 }
 
-// offsets nondecreasing within [0, n]; labels of rows inside a sequence below V (negative ones do not count)
 __global__ __launch_bounds__(256) void check_preference_kernel(PrefArgs p) {
-  const int sequences = 2 * p.pairs;
-  const int64_t first = p.offsets[0], last = p.offsets[sequences];
-  const int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
-  uint32_t bad = 0;
-  for (int64_t i = i0; i <= sequences; i += step) {
-    const int64_t v = p.offsets[i];
-    if (v < 0 || v > p.n || (i < sequences && p.offsets[i + 1] < v)) bad |= OPS_BAD_OFFSETS;
-  }
-  for (int64_t t = i0; t < p.n; t += step)
-    if (t >= first && t < last && p.labels[t] >= p.V) bad |= OPS_BAD_LABEL;
+  uint32_t bad = bad_args(p, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) bad |= (uint32_t)__shfl_xor((int)bad, o, 64);
   if (bad && (threadIdx.x & 63) == 0) atomicOr(p.bad, bad);
@@ -355,15 +371,29 @@ void launch_loss_typed(const PrefArgs& p, hipStream_t s) {
   pair_loss_kernel<TYPE, false><<<p.pairs, p.n / p.pairs > 8192 ? 1024 : 256, 0, s>>>(p);
 }
 
+// Up to so many rows and sequences every workgroup of the gradient checks them all, a few loads a thread, which saves the
+// launch of a kernel ahead of it (2.5 of a small call's 20 us).
+constexpr int64_t kCheckHere = 512;
+
+template <int TYPE, bool WAVE>
+void launch_gradient(const PrefArgs& p, int64_t blocks, hipStream_t s) {
+  if (p.n <= kCheckHere && 2 * (int64_t)p.pairs <= kCheckHere) {
+    preference_backward_kernel<TYPE, WAVE, true><<<(unsigned)blocks, 256, 0, s>>>(p);
+  } else {
+    check(p, s);
+    preference_backward_kernel<TYPE, WAVE, false><<<(unsigned)blocks, 256, 0, s>>>(p);
+  }
+}
+
 template <int TYPE>
 void launch_backward_typed(PrefArgs p, hipStream_t s) {
-  check(p, s);
+  const int64_t rows = std::max<int64_t>(p.n, 1);
   if (p.V <= kWaveRow) {
-    preference_backward_kernel<TYPE, true><<<(unsigned)((std::max<int64_t>(p.n, 1) + 3) / 4), 256, 0, s>>>(p);
+    launch_gradient<TYPE, true>(p, (rows + 3) / 4, s);
   } else {
     // four workgroups and more on each of the 256 compute units where there are few rows
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.V / 2048, 2048 / std::max<int64_t>(p.n, 1)));
-    preference_backward_kernel<TYPE, false><<<(unsigned)(std::max<int64_t>(p.n, 1) * p.splits), 256, 0, s>>>(p);
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.V / 2048, 2048 / rows));
+    launch_gradient<TYPE, false>(p, rows * p.splits, s);
   }
 }
 

@@ -133,6 +133,7 @@ void place_plan(GroupPlan* plan, char* p, int64_t m, int64_t k) {
   plan->partial = (float*)p;
   p += (size_t)plan->partial_slots * m * k * 4;
   p = (char*)(((uintptr_t)p + 15) & ~(uintptr_t)15);
+  if (!plan->tables) return;
   plan->rows.at = (int4*)p;
   plan->da.at = plan->rows.at + plan->rows.count;
   plan->join = plan->da.at + plan->da.count;
