@@ -57,8 +57,7 @@ void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, i
 // up to three operands into rows of wp values, a multiple of 16 bytes, zeros behind `width`
 void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,
                        const int64_t* rows, const int* width, const int* wp, hipStream_t s);
-// false: the grid would not fit
-bool launch_group_product(const GroupArgs& g, int type, int which, const GroupPlan& p, hipStream_t s);
+void launch_group_product(const GroupArgs& g, int type, int which, const GroupPlan& p, hipStream_t s);
 
 // ---- preference loss ----------------------------------------------------------------------------
 struct PrefArgs {

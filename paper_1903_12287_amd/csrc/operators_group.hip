@@ -19,7 +19,8 @@ using tile::KR;
 struct Launch {
   const int4* slots;          // NULL: up to 63 groups, every wave finds its slot itself
   int shift;                  // rows of a slot: 2^shift
-  int row_tiles, col_tiles;   // da: tiles of one matrix; y, dx: slots of all groups, tiles of the columns
+  int64_t first;              // this launch's first slot
+  int row_tiles, col_tiles;   // da: tiles of one matrix; y, dx: slots of the launch, tiles of the columns
   uint32_t blocks;
   float* partial;             // da: partial sums of the groups of several slots
   const int4* join;
@@ -32,7 +33,6 @@ struct Launch {
 // ceil(L / 2^shift) of them, so that 2 n / 2^shift places are enough, however many groups there are.
 __device__ __forceinline__ int64_t first_slot(int64_t offset, int g, int shift) { return (offset >> shift) + g; }
 __device__ __forceinline__ int64_t first_place(int64_t offset, int shift) { return (2 * offset) >> shift; }
-
 
 // slot v of slots of 2^shift rows, where group g holds rows [first, last) and slot v is at or behind its first slot
 __device__ __forceinline__ int4 slot_in(int g, int64_t first, int64_t last, int shift, int64_t v, bool places) {
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(64 * WM * WN) void group_rows_kernel(GroupArgs g, L
   band_tile<BAND>(at, L.row_tiles, L.col_tiles, slot, col);
   const int j0 = (int)col * BN;
   int4 at_slot;
-  if (!find_slot(g, L, slot, false, at_slot)) return;
+  if (!find_slot(g, L, L.first + slot, false, at_slot)) return;
   const int64_t r0 = at_slot.x;
   const int rows = at_slot.y, grp = at_slot.z;
   if (rows <= 0) return;
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Lau
   const uint32_t at = tile::xcd_place(blockIdx.x, L.blocks);
   const int tiles = L.row_tiles * L.col_tiles;
   int4 slot;
-  if (!find_slot(g, L, at / tiles, true, slot)) return;
+  if (!find_slot(g, L, L.first + at / tiles, true, slot)) return;
   const int t = (int)(at % tiles);
   const int i0 = t / L.col_tiles * BM, j0 = t % L.col_tiles * BN;
   if (slot.z < 0) return;   // the first slot of an empty group stores zeros
@@ -219,9 +219,8 @@ struct PackArgs {
   int64_t ld[3], rows[3];
   int width[3], wp[3];
   uint32_t first[4];   // first workgroup of each
+  int64_t per;         // rows of a workgroup
 };
-
-constexpr int kPackRows = 16;
 
 template <int TYPE>
 __global__ __launch_bounds__(256) void group_pack_kernel(PackArgs a) {
@@ -229,8 +228,8 @@ __global__ __launch_bounds__(256) void group_pack_kernel(PackArgs a) {
   typedef typename Vec<TYPE>::V V;
   constexpr int N = Vec<TYPE>::N;
   const int w = blockIdx.x >= a.first[2] ? 2 : (blockIdx.x >= a.first[1] ? 1 : 0);
-  const int64_t r0 = (int64_t)(blockIdx.x - a.first[w]) * kPackRows;
-  const int64_t r1 = min(a.rows[w], r0 + kPackRows);
+  const int64_t r0 = (int64_t)(blockIdx.x - a.first[w]) * a.per;
+  const int64_t r1 = min(a.rows[w], r0 + a.per);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   for (int64_t r = r0 + wave; r < r1; r += 4) {
     const T* s = (const T*)a.src[w] + r * a.ld[w];
@@ -249,38 +248,41 @@ __global__ __launch_bounds__(256) void group_pack_kernel(PackArgs a) {
 // ---- what is launched ------------------------------------------------------------------------------
 int64_t tiles_of(int64_t v, int b) { return (v + b - 1) / b; }
 
+// a launch takes so many workgroups; of more, the slots are launched in turn
+constexpr int64_t kLaunch = 1 << 22;
+
 template <int TYPE, int WHICH, int BM, int BN, int WM, int WN>
-bool launch_rows(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) {
+void launch_rows(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) {
   L.slots = p.rows.at;
   L.shift = p.rows.shift;
-  L.row_tiles = (int)p.rows.count;
   L.col_tiles = (int)tiles_of(WHICH == GP_FORWARD ? g.m : g.k, BN);
-  const int64_t blocks = p.rows.count * L.col_tiles;
-  if (blocks * 64 * WM * WN >= 1ll << 32) return false;
-  L.blocks = (uint32_t)blocks;
-  group_rows_kernel<TYPE, WHICH, BM, BN, WM, WN><<<L.blocks, 64 * WM * WN, 0, s>>>(g, L);
-  return true;
+  const int64_t step = kLaunch / L.col_tiles;   // col_tiles <= 1024
+  for (L.first = 0; L.first < p.rows.count; L.first += step) {
+    L.row_tiles = (int)std::min(step, p.rows.count - L.first);
+    L.blocks = (uint32_t)L.row_tiles * L.col_tiles;
+    group_rows_kernel<TYPE, WHICH, BM, BN, WM, WN><<<L.blocks, 64 * WM * WN, 0, s>>>(g, L);
+  }
 }
 
 template <int TYPE, int B>
-bool launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) {
+void launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) {
   L.slots = p.da.at;
   L.shift = p.da.shift;
   L.partial = p.partial;
   L.join = p.join;
   L.row_tiles = (int)tiles_of(g.m, B);
   L.col_tiles = (int)tiles_of(g.k, B);
-  const int64_t blocks = p.da.count * L.row_tiles * L.col_tiles;
-  if (blocks * 256 >= 1ll << 32) return false;
-  L.blocks = (uint32_t)blocks;
-  group_da_kernel<TYPE, B, B, 2, 2><<<L.blocks, 256, 0, s>>>(g, L);
+  const int64_t tiles = (int64_t)L.row_tiles * L.col_tiles, step = kLaunch / tiles;   // 1,024 x 1,024 tiles at most
+  for (L.first = 0; L.first < p.da.count; L.first += step) {
+    L.blocks = (uint32_t)(std::min(step, p.da.count - L.first) * tiles);
+    group_da_kernel<TYPE, B, B, 2, 2><<<L.blocks, 256, 0, s>>>(g, L);
+  }
   if (p.joins > 0) {
     // most entries are groups of one slot, whose workgroups end at once: 16,384 in all
     const int64_t chunks = std::max<int64_t>(64, 16384 / p.joins);
     const dim3 grid((unsigned)std::min(tiles_of((int64_t)g.m * g.k, 64), chunks), (unsigned)p.joins);
     group_join_kernel<TYPE><<<grid, 256, 0, s>>>(g, L);
   }
-  return true;
 }
 
 // Rows and columns of a tile of da: in float32 the matrix unit sets the time, and more, smaller workgroups keep it busier
@@ -304,7 +306,7 @@ int row_shift(int type, int64_t n, int groups, int64_t cols) {
 }
 
 template <int TYPE, int WHICH>
-bool launch_rows_by_size(const GroupArgs& g, const GroupPlan& p, const Launch& L, hipStream_t s) {
+void launch_rows_by_size(const GroupArgs& g, const GroupPlan& p, const Launch& L, hipStream_t s) {
   if constexpr (TYPE != OT_F32) {
     if (p.rows.shift == 8) return launch_rows<TYPE, WHICH, 256, 256, 2, 4>(g, p, L, s);
   }
@@ -313,7 +315,7 @@ bool launch_rows_by_size(const GroupArgs& g, const GroupPlan& p, const Launch& L
 }
 
 template <int TYPE>
-bool launch_typed(const GroupArgs& g, int which, const GroupPlan& p, hipStream_t s) {
+void launch_typed(const GroupArgs& g, int which, const GroupPlan& p, hipStream_t s) {
   Launch L{};
   if (which == GP_DA) return launch_da<TYPE, da_tile(TYPE)>(g, p, L, s);
   if (which == GP_FORWARD) return launch_rows_by_size<TYPE, GP_FORWARD>(g, p, L, s);
@@ -413,6 +415,10 @@ GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int6
 void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,
                        const int64_t* rows, const int* width, const int* wp, hipStream_t s) {
   PackArgs a{};
+  int64_t total = 0;
+  for (int i = 0; i < count; ++i) total += rows[i];
+  a.per = 16;
+  while (total / a.per > kLaunch) a.per *= 2;
   uint32_t at = 0;
   for (int i = 0; i < 3; ++i) {
     a.first[i] = at;
@@ -423,7 +429,7 @@ void launch_group_pack(int type, int count, const void* const* src, void* const*
     a.rows[i] = rows[i];
     a.width[i] = width[i];
     a.wp[i] = wp[i];
-    at += (uint32_t)tiles_of(rows[i], kPackRows);
+    at += (uint32_t)((rows[i] + a.per - 1) / a.per);
   }
   if (!at) return;
   if (type == OT_F32) group_pack_kernel<OT_F32><<<at, 256, 0, s>>>(a);
@@ -431,7 +437,7 @@ void launch_group_pack(int type, int count, const void* const* src, void* const*
   else group_pack_kernel<OT_F16><<<at, 256, 0, s>>>(a);
 }
 
-bool launch_group_product(const GroupArgs& g, int type, int which, const GroupPlan& p, hipStream_t s) {
+void launch_group_product(const GroupArgs& g, int type, int which, const GroupPlan& p, hipStream_t s) {
   switch (type) {
     case OT_F32: return launch_typed<OT_F32>(g, which, p, s);
     case OT_BF16: return launch_typed<OT_BF16>(g, which, p, s);

@@ -190,10 +190,7 @@ extern "C" pbg_status pbg_group_linear(pbg_ctx* ctx, int32_t dtype, const void* 
   launch_group_pack(dtype, ops.count, ops.src, ops.dst, ops.ld, ops.rows, ops.width, ops.wp, ctx->cs);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) {
-    if (!launch_group_product(g, dtype, GP_FORWARD, plan, ctx->cs)) {
-      (void)hipStreamSynchronize(ctx->cs);
-      return set_err(ctx, PBG_ERR_UNSUPPORTED, "more tiles than a launch holds");
-    }
+    launch_group_product(g, dtype, GP_FORWARD, plan, ctx->cs);
     e = hipGetLastError();
   }
   return end_call(ctx, e, "pbg_group_linear");
@@ -243,22 +240,17 @@ extern "C" pbg_status pbg_group_linear_backward(pbg_ctx* ctx, int32_t dtype, con
   launch_group_plan(plan, offsets, groups, n, ctx->edge_flag, ctx->cs);
   launch_group_pack(dtype, ops.count, ops.src, ops.dst, ops.ld, ops.rows, ops.width, ops.wp, ctx->cs);
   hipError_t e = hipGetLastError();
-  bool fits = true;
   if (e == hipSuccess && dx) {
     g.out = dx;
     g.ldo = lddx;
-    fits = launch_group_product(g, dtype, GP_DX, plan, ctx->cs);
+    launch_group_product(g, dtype, GP_DX, plan, ctx->cs);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && fits && da) {
+  if (e == hipSuccess && da) {
     g.out = da;
     g.ldo = in_dim;
-    fits = launch_group_product(g, dtype, GP_DA, plan, ctx->cs);
+    launch_group_product(g, dtype, GP_DA, plan, ctx->cs);
     e = hipGetLastError();
-  }
-  if (!fits) {
-    (void)hipStreamSynchronize(ctx->cs);
-    return set_err(ctx, PBG_ERR_UNSUPPORTED, "more tiles than a launch holds");
   }
   return end_call(ctx, e, "pbg_group_linear_backward");
 }
@@ -387,6 +379,7 @@ extern "C" pbg_status pbg_clip_gradients(pbg_ctx* ctx, int32_t num_tensors, cons
   if (!(max_norm > 0.0)) return set_err(ctx, PBG_ERR_INVALID_ARG, "max_norm must be above 0");
   if (num_tensors > 0 && (!dtypes_host || !counts_host || !grads_host))
     return set_err(ctx, PBG_ERR_INVALID_ARG, "NULL array");
+  constexpr int64_t kMaxValues = 1ll << 38;   // of all tensors together, more than the memory holds
   try {
     struct Range {
       uintptr_t begin, end;
@@ -396,7 +389,11 @@ extern "C" pbg_status pbg_clip_gradients(pbg_ctx* ctx, int32_t num_tensors, cons
     std::vector<ClipBatch> batches;
     ranges.reserve((size_t)num_tensors * 2);
     int64_t blocks = 0, values = 0;
-    for (int32_t i = 0; i < num_tensors; ++i) values += counts_host[i] > 0 ? counts_host[i] : 0;
+    for (int32_t i = 0; i < num_tensors; ++i) {
+      if (counts_host[i] < 0 || counts_host[i] > kMaxValues - values)
+        return set_err(ctx, PBG_ERR_INVALID_ARG, "count %d out of range", i);
+      values += counts_host[i];
+    }
     // one workgroup's sum adds all parts: at most about 16,384 of them (75,700 parts of 8,192 values took it 24 us)
     int64_t span = kClipBlock;
     while (values / span > 16384) span *= 2;
@@ -404,7 +401,6 @@ extern "C" pbg_status pbg_clip_gradients(pbg_ctx* ctx, int32_t num_tensors, cons
       const int64_t c = counts_host[i];
       const int32_t ty = dtypes_host[i];
       if (ty < PBG_TYPE_F32 || ty > PBG_TYPE_F16) return set_err(ctx, PBG_ERR_INVALID_ARG, "unknown type %d", ty);
-      if (c < 0 || c > (1ll << 38)) return set_err(ctx, PBG_ERR_INVALID_ARG, "count %d out of range", i);
       if (c == 0) continue;
       const int es = type_bytes(ty);
       const void* g = grads_host[i];

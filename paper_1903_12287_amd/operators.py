@@ -86,17 +86,27 @@ def _vector(t, dtype, n, what, allow_none=False):
     return pbg._ptr(t, dtype, what, allow_none=allow_none)
 
 
+def _here(*tensors):
+    """The context's device is the current one, and so must the tensors' be."""
+    d = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != d:
+            raise ValueError(f"a tensor is on device {t.get_device()}, the current device is {d}")
+
+
 def _values(tensors, what):
     """Types, numbers of values and pointers of contiguous device tensors of any shapes (an attribute at a time over
     all of them: half the time of a loop over tensors)."""
     try:
         types = [TYPES[t.dtype] for t in tensors]
-        if all([t.is_cuda for t in tensors]) and all([t.is_contiguous() for t in tensors]):
+        d = {t.get_device() for t in tensors}   # -1: the host
+        if (not d or d == {torch.cuda.current_device()}) and all([t.is_contiguous() for t in tensors]):
             return types, [t.numel() for t in tensors], [t.data_ptr() for t in tensors]
-    except (KeyError, AttributeError):
+    except (KeyError, AttributeError, RuntimeError):   # the last: no device at all
         pass
     for i, t in enumerate(tensors):   # which one, and why
         pbg._ptr(t, _type(t, f"{what}[{i}]"), f"{what}[{i}]")
+        _here(t)
     raise TypeError(f"{what} must be tensors")
 
 
@@ -117,9 +127,9 @@ def pbg_group_linear(ctx, x, a, offsets, y):
     n = x.shape[0]
     xp, ldx = _rows(x, dt, (n, k), "x")
     yp, ldy = _rows(y, dt, (n, m), "y")
-    _check(ctx, library().pbg_group_linear(ctx, TYPES[dt], xp, ldx, ap,
-                                           _vector(offsets, torch.int64, groups + 1, "offsets"), groups, n, k, m, yp,
-                                           ldy))
+    op = _vector(offsets, torch.int64, groups + 1, "offsets")
+    _here(x, a, offsets, y)
+    _check(ctx, library().pbg_group_linear(ctx, TYPES[dt], xp, ldx, ap, op, groups, n, k, m, yp, ldy))
 
 
 def pbg_group_linear_backward(ctx, x, a, offsets, dy, dx=None, da=None):
@@ -140,9 +150,10 @@ def pbg_group_linear_backward(ctx, x, a, offsets, dy, dx=None, da=None):
     dyp, lddy = _rows(dy, dt, (n, m), "dy")
     if n and ((dx is not None and a is None) or (da is not None and x is None)):
         raise ValueError("dx needs a, da needs x")
-    _check(ctx, library().pbg_group_linear_backward(
-        ctx, TYPES[dt], xp, ldx, ap, dyp, lddy, _vector(offsets, torch.int64, groups + 1, "offsets"), groups, n, k, m,
-        dxp, lddx, dap))
+    op = _vector(offsets, torch.int64, groups + 1, "offsets")
+    _here(x, a, offsets, dy, dx, da)
+    _check(ctx, library().pbg_group_linear_backward(ctx, TYPES[dt], xp, ldx, ap, dyp, lddy, op, groups, n, k, m, dxp,
+                                                    lddx, dap))
 
 
 def pbg_preference_loss(ctx, logits, labels, offsets, ref_logp, beta, smoothing, loss, logp, dlogp, row_stats):
@@ -155,12 +166,12 @@ def pbg_preference_loss(ctx, logits, labels, offsets, ref_logp, beta, smoothing,
     pairs = (offsets.numel() - 1) // 2
     lp, ld = _rows(logits, dt, (n, cands), "logits")
     f = torch.float32
-    _check(ctx, library().pbg_preference_loss(
-        ctx, TYPES[dt], lp, ld, _vector(labels, torch.int32, n, "labels"),
-        _vector(offsets, torch.int64, 2 * pairs + 1, "offsets"), pairs, n, cands,
-        _vector(ref_logp, f, 2 * pairs, "ref_logp", True), float(beta), float(smoothing),
-        _vector(loss, f, pairs, "loss", True), _vector(logp, f, 2 * pairs, "logp"),
-        _vector(dlogp, f, 2 * pairs, "dlogp", True), _vector(row_stats, f, 2 * n, "row_stats")))
+    args = (_vector(labels, torch.int32, n, "labels"), _vector(offsets, torch.int64, 2 * pairs + 1, "offsets"), pairs,
+            n, cands, _vector(ref_logp, f, 2 * pairs, "ref_logp", True), float(beta), float(smoothing),
+            _vector(loss, f, pairs, "loss", True), _vector(logp, f, 2 * pairs, "logp"),
+            _vector(dlogp, f, 2 * pairs, "dlogp", True), _vector(row_stats, f, 2 * n, "row_stats"))
+    _here(logits, labels, offsets, ref_logp, loss, logp, dlogp, row_stats)
+    _check(ctx, library().pbg_preference_loss(ctx, TYPES[dt], lp, ld, *args))
 
 
 def pbg_preference_loss_backward(ctx, logits, labels, offsets, row_stats, dlogp, dlogits):
@@ -173,10 +184,10 @@ def pbg_preference_loss_backward(ctx, logits, labels, offsets, row_stats, dlogp,
     lp, ld = _rows(logits, dt, (n, cands), "logits")
     dp, lddl = _rows(dlogits, dt, (n, cands), "dlogits")
     f = torch.float32
-    _check(ctx, library().pbg_preference_loss_backward(
-        ctx, TYPES[dt], lp, ld, _vector(labels, torch.int32, n, "labels"),
-        _vector(offsets, torch.int64, 2 * pairs + 1, "offsets"), pairs, n, cands,
-        _vector(row_stats, f, 2 * n, "row_stats"), _vector(dlogp, f, 2 * pairs, "dlogp"), dp, lddl))
+    args = (_vector(labels, torch.int32, n, "labels"), _vector(offsets, torch.int64, 2 * pairs + 1, "offsets"), pairs,
+            n, cands, _vector(row_stats, f, 2 * n, "row_stats"), _vector(dlogp, f, 2 * pairs, "dlogp"))
+    _here(logits, labels, offsets, row_stats, dlogp, dlogits)
+    _check(ctx, library().pbg_preference_loss_backward(ctx, TYPES[dt], lp, ld, *args, dp, lddl))
 
 
 def pbg_clip_gradients(ctx, grads, max_norm, outs=None) -> float:
