@@ -42,6 +42,7 @@ struct GroupPlan {
   bool tables;             // the tables below are written ahead of the products (else their pointers are NULL)
   GroupSlots rows;         // y, dx: a slot's rows are a tile's
   GroupSlots da;           // da: a slot's rows are summed by one workgroup
+  int da_tile;             // rows and columns of a tile of da
   int64_t partial_slots;   // places of partial sums, m k floats each (0: no group is longer than a slot)
   float* partial;
   int64_t joins;           // entries of the table of groups of several sums: by group or by place, whichever are fewer

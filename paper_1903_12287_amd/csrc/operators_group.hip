@@ -21,7 +21,7 @@ struct Launch {
   int shift;                  // rows of a slot: 2^shift
   int64_t first;              // this launch's first slot
   int row_tiles, col_tiles;   // da: tiles of one matrix; y, dx: slots of the launch, tiles of the columns
-  uint32_t blocks;
+  uint32_t blocks, chunk;
   float* partial;             // da: partial sums of the groups of several slots
   const int4* join;
 };
@@ -134,8 +134,12 @@ __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Lau
   typedef tile::Tile<TYPE, KR, KR, BM, BN, WM, WN> Tl;
   constexpr int ES = TYPE == OT_F32 ? 4 : 2;
   __shared__ __attribute__((aligned(1024))) char lds0[Tl::STAGE], lds1[Tl::STAGE];
-  const uint32_t at = tile::xcd_place(blockIdx.x, L.blocks);
+  // The tiles of a slot in chunks, which the XCDs take in turn: one XCD's workgroups share operands, and every XCD gets
+  // a part of each long slot.
   const int tiles = L.row_tiles * L.col_tiles;
+  const uint32_t j = blockIdx.x >> 3, chunk = j / L.chunk;
+  const uint32_t at = (chunk * 8 + (blockIdx.x & 7)) * L.chunk + (j - chunk * L.chunk);
+  if (at >= L.blocks) return;
   int4 slot;
   if (!find_slot(g, L, L.first + at / tiles, true, slot)) return;
   const int t = (int)(at % tiles);
@@ -275,7 +279,12 @@ void launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) 
   const int64_t tiles = (int64_t)L.row_tiles * L.col_tiles, step = kLaunch / tiles;   // 1,024 x 1,024 tiles at most
   for (L.first = 0; L.first < p.da.count; L.first += step) {
     L.blocks = (uint32_t)(std::min(step, p.da.count - L.first) * tiles);
-    group_da_kernel<TYPE, B, B, 2, 2><<<L.blocks, 256, 0, s>>>(g, L);
+    // An eighth of a slot, where that is tiles enough to share operands; else an eighth of them all.  (Eighths of them all
+    // whatever the tiles: 32 groups, 65,536 rows, the longest group 3 times the average, 2,048 x 2,048: 817 us for 566.)
+    L.chunk = (uint32_t)(tiles >= 64 ? tiles / 8 : tiles_of(L.blocks, 8));
+    const unsigned grid = (unsigned)(tiles_of(L.blocks, 8 * (int)L.chunk) * 8 * L.chunk);
+    constexpr int WN = B == 256 ? 4 : 2;
+    group_da_kernel<TYPE, B, B, 2, WN><<<grid, 128 * WN, 0, s>>>(g, L);
   }
   if (p.joins > 0) {
     // most entries are groups of one slot, whose workgroups end at once: 16,384 in all
@@ -286,9 +295,13 @@ void launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) 
 }
 
 // Rows and columns of a tile of da: in float32 the matrix unit sets the time, and more, smaller workgroups keep it busier
-// (8 groups, 40,000 rows, 100 x 100: both gradients 70 us for 75); in 16 bits reading the operands does (32 groups,
-// 16,384 rows, 2,048 x 2,048: 524 us for 448).
-constexpr int da_tile(int type) { return type == OT_F32 ? 64 : 128; }
+// (8 groups, 40,000 rows, 100 x 100: both gradients 70 us for 75); in 16 bits reading the operands does (128 x 128 / 256 x
+// 256, of 2,048 x 2,048: 32 groups of 512 rows 267 / 248 us, of 2,048 rows 610 / 535, uneven ones 672 / 566; where
+// groups have to be cut to give every compute unit a tile, 4 groups of 4,096 rows: 153 / 258).
+int da_tile(int type, int64_t n, int64_t groups, int64_t m, int64_t k) {
+  if (type == OT_F32) return 64;
+  return n / groups >= 512 && groups * tiles_of(m, 256) * tiles_of(k, 256) >= 512 ? 256 : 128;
+}
 
 // Rows of a tile of y or dx, 2^shift, by the average group and the number of tiles.  Measured (us, 32 x 64 / 128 x 128 /
 // 256 x 256 tiles):
@@ -317,7 +330,14 @@ void launch_rows_by_size(const GroupArgs& g, const GroupPlan& p, const Launch& L
 template <int TYPE>
 void launch_typed(const GroupArgs& g, int which, const GroupPlan& p, hipStream_t s) {
   Launch L{};
-  if (which == GP_DA) return launch_da<TYPE, da_tile(TYPE)>(g, p, L, s);
+  if (which == GP_DA) {
+    if constexpr (TYPE == OT_F32) {
+      return launch_da<TYPE, 64>(g, p, L, s);
+    } else {
+      if (p.da_tile == 256) return launch_da<TYPE, 256>(g, p, L, s);
+      return launch_da<TYPE, 128>(g, p, L, s);
+    }
+  }
   if (which == GP_FORWARD) return launch_rows_by_size<TYPE, GP_FORWARD>(g, p, L, s);
   return launch_rows_by_size<TYPE, GP_DX>(g, p, L, s);
 }
@@ -398,7 +418,8 @@ GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int6
   if (!want_da) return p;
   // Rows of a slot of da: enough slots for a few workgroups on each of the 256 compute units, where the matrices' tiles
   // alone are not; with tiles enough, only groups of four times the average and more are cut.
-  const int64_t tiles = tiles_of(m, da_tile(type)) * tiles_of(k, da_tile(type));
+  p.da_tile = da_tile(type, n, groups, m, k);
+  const int64_t tiles = tiles_of(m, p.da_tile) * tiles_of(k, p.da_tile);
   int64_t rows = std::max<int64_t>(128, n * tiles / 1024);
   if (groups * tiles >= 512) rows = std::max(rows, 4 * n / groups);
   int shift = 7;

@@ -203,6 +203,13 @@ struct Tile {
       for (int j = 0; j < JB; ++j) acc[i][j] = (v4f){0.f, 0.f, 0.f, 0.f};
     const int nk = (int)((depth + 2 * KS - 1) / (2 * KS)) * 2;   // an even number of slices
     if (nk == 0) return;
+    if constexpr (NW == 8 && MP == KR) {
+      fetch(lds0, op, oq, 0);
+      if (wm * IB * 16 >= rows || wn * JB * 16 >= cols) turns<0>(lds0, lds1, op, oq, nk, w >= 4, acc);
+      else turns<IB>(lds0, lds1, op, oq, nk, w >= 4, acc);
+      pieces::wait_loads();
+      return;
+    }
     fetch(lds0, op, oq, 0);
     fetch(lds1, op, oq, 1);
     stage_barrier<FETCHES>();    // slice 0 has landed
@@ -228,6 +235,70 @@ struct Tile {
   __device__ __forceinline__ static void fetch(lds_t* stage, const P& op, const Q& oq, int kt) {
     op.fetch(stage, 0, kt);
     oq.fetch(stage, P::BYTES, kt);
+  }
+
+  // The products by eight waves, two on each of the four units, which take turns: one reads half a slice while the other
+  // multiplies its half; a slice is four turns, the second wave a turn behind.  Half as many registers hold what was
+  // read, which two KR operands at 256 x 256 need.  (Where both fit, slices() is faster by 0 to 5 %: a fetch has a slice
+  // and a half to arrive there, one here.)  IA 0: the wave only moves its share.
+  template <int IA>
+  __device__ __forceinline__ static void turns(lds_t* lds0, lds_t* lds1, const P& op, const Q& oq, int nk, bool second,
+                                               v4f (&acc)[IB][JB]) {
+    typename Mfma<TYPE>::Frag fp[IA < 1 ? 1 : IA], fq[JB];
+    auto read = [&](const lds_t* stage, int s) {
+      if (IA == 0) return;
+#pragma unroll
+      for (int j = 0; j < JB; ++j) fq[j] = oq.read(stage, P::BYTES, j, s);
+#pragma unroll
+      for (int i = 0; i < IA; ++i) fp[i] = op.read(stage, 0, i, s);
+    };
+    auto multiply = [&]() {
+#pragma unroll
+      for (int r = 0; r < Mfma<TYPE>::SUB; ++r)
+#pragma unroll
+        for (int i = 0; i < IA; ++i)
+#pragma unroll
+          for (int j = 0; j < JB; ++j) acc[i][j] = Mfma<TYPE>::mul(fq[j], fp[i], acc[i][j], r);
+    };
+    stage_barrier<0>();            // slice 0 has landed
+    if (second) {
+      fetch(lds1, op, oq, 1);
+      stage_barrier<FETCHES>();
+      auto slice = [&](lds_t* now, int kt) {
+        read(now, 0);
+        stage_barrier<FETCHES>();
+        multiply();
+        stage_barrier<FETCHES>();
+        read(now, 1);
+        stage_barrier<0>();        // slice kt + 1 has landed, and everyone has read this one
+        fetch(now, op, oq, kt + 2);
+        multiply();
+        if (IA > 0) interleave<0, FETCHES, IA * JB>();
+        stage_barrier<FETCHES>();
+      };
+      for (int kt = 0; kt < nk; kt += 2) {
+        slice(lds0, kt);
+        slice(lds1, kt + 1);
+      }
+    } else {
+      auto slice = [&](lds_t* now, lds_t* next, int kt) {
+        read(now, 0);
+        stage_barrier<FETCHES>();
+        fetch(next, op, oq, kt + 1);   // read by everyone before this slice
+        multiply();
+        if (IA > 0) interleave<0, FETCHES, IA * JB>();
+        stage_barrier<FETCHES>();
+        read(now, 1);
+        stage_barrier<FETCHES>();
+        multiply();
+        stage_barrier<0>();        // slice kt + 1 has landed
+      };
+      for (int kt = 0; kt < nk; kt += 2) {
+        slice(lds0, lds1, kt);
+        slice(lds1, lds0, kt + 1);
+      }
+      stage_barrier<0>();
+    }
   }
 
   // the wave's products over nk slices, of its first IA row blocks

@@ -188,3 +188,20 @@ def test_two_contexts_at_once():
             assert all(torch.equal(p, q) for p, q in zip(r, alone[i]))
     for c in contexts:
         pbg.pbg_free(c)
+
+
+@pytest.mark.parametrize("sizes,k,m", [([600] * 7 + [4000, 0], 2048, 2048),    # wide tiles, one group longer than a slot
+                                       ([513, 700, 499] * 19 + [2500], 500, 1000),   # matrices that end inside a tile
+                                       ([900] * 4, 264, 520), ([64, 0, 1], 1030, 1040)])
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16])
+def test_gradients_of_large_matrices(ctx, sizes, k, m, t):
+    n, groups = sum(sizes), len(sizes)
+    x, dy = small_integers(8, n, k, dtype=t), small_integers(9, n, m, dtype=t)
+    # sums of whole numbers below 2^24: exact in float32 in any order
+    off = torch.tensor(np.concatenate([[0], np.cumsum(sizes)]), dtype=torch.int64, device="cuda")
+    da = torch.full((groups, m, k), 9.0, dtype=t, device="cuda")
+    ops.pbg_group_linear_backward(ctx, x, None, off, dy, None, da)
+    for g in range(groups):
+        r = slice(int(off[g]), int(off[g + 1]))
+        exact = dy[r].float().t().contiguous() @ x[r].float()
+        assert torch.equal(da[g], exact.to(t))
