@@ -279,9 +279,10 @@ void launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) 
   const int64_t tiles = (int64_t)L.row_tiles * L.col_tiles, step = kLaunch / tiles;   // 1,024 x 1,024 tiles at most
   for (L.first = 0; L.first < p.da.count; L.first += step) {
     L.blocks = (uint32_t)(std::min(step, p.da.count - L.first) * tiles);
-    // An eighth of a slot, where that is tiles enough to share operands; else an eighth of them all.  (Eighths of them all
-    // whatever the tiles: 32 groups, 65,536 rows, the longest group 3 times the average, 2,048 x 2,048: 817 us for 566.)
-    L.chunk = (uint32_t)(tiles >= 64 ? tiles / 8 : tiles_of(L.blocks, 8));
+    // An eighth of a slot, where that is tiles enough to share operands, else a slot.  (Eighths of all tiles in a row:
+    // bfloat16, 32 groups, 65,536 rows, the longest group 3 times the average, 2,048 x 2,048: 817 us for 566; float32,
+    // 1,345 groups, 40,000 rows, sizes as 1 / rank, 400 x 400: 860 for 500.)
+    L.chunk = (uint32_t)(tiles >= 64 ? tiles / 8 : tiles);
     const unsigned grid = (unsigned)(tiles_of(L.blocks, 8 * (int)L.chunk) * 8 * L.chunk);
     constexpr int WN = B == 256 ? 4 : 2;
     group_da_kernel<TYPE, B, B, 2, WN><<<grid, 128 * WN, 0, s>>>(g, L);
@@ -420,8 +421,8 @@ GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int6
   // alone are not; with tiles enough, only groups of four times the average and more are cut.
   p.da_tile = da_tile(type, n, groups, m, k);
   const int64_t tiles = tiles_of(m, p.da_tile) * tiles_of(k, p.da_tile);
-  int64_t rows = std::max<int64_t>(128, n * tiles / 1024);
-  if (groups * tiles >= 512) rows = std::max(rows, 4 * n / groups);
+  int64_t rows = std::max<int64_t>(256, n * tiles / 1024);
+  if (groups * tiles >= 512) rows = std::max(rows, (type == OT_F32 ? 1 : 4) * n / groups);
   int shift = 7;
   while (shift < 31 && ((int64_t)1 << shift) < rows) ++shift;
   // the partial sums stay below 512 MB, and a grid has 65,535 of them
