@@ -21,7 +21,7 @@ struct Launch {
   int shift;                  // rows of a slot: 2^shift
   int64_t first;              // this launch's first slot
   int row_tiles, col_tiles;   // da: tiles of one matrix; y, dx: slots of the launch, tiles of the columns
-  uint32_t blocks, chunk;
+  uint32_t blocks, band, chunk;   // tiles; the order in which they are taken
   float* partial;             // da: partial sums of the groups of several slots
   const int4* join;
 };
@@ -90,14 +90,22 @@ __device__ __forceinline__ bool find_slot(const GroupArgs& g, const Launch& L, i
   return true;
 }
 
-// Tiles in bands of BAND slots, column by column: the workgroups that an XCD runs at a time share the rows of a few
+// Tiles in bands of `band` slots, column by column: the workgroups that an XCD runs at a time share the rows of a few
 // slots and the matrix rows of a few columns, which its L2 then fetches once.
-template <int BAND>
-__device__ __forceinline__ void band_tile(uint32_t at, uint32_t slots, uint32_t cols, uint32_t& slot, uint32_t& col) {
-  const uint32_t band = at / (BAND * cols), r = at - band * (BAND * cols);
-  const uint32_t h = min((uint32_t)BAND, slots - BAND * band);
+__device__ __forceinline__ void band_tile(uint32_t at, uint32_t band, uint32_t slots, uint32_t cols, uint32_t& slot,
+                                          uint32_t& col) {
+  const uint32_t b = at / (band * cols), r = at - b * (band * cols);
+  const uint32_t h = min(band, slots - band * b);
   col = r / h;
-  slot = BAND * band + (r - col * h);
+  slot = band * b + (r - col * h);
+}
+
+// Hardware hands workgroups to the eight XCDs in turn, each with an L2 of its own: the tile of this workgroup such that
+// the XCDs take chunks of L.chunk tiles in turn.  Tiles in a chunk share operands; and every XCD gets its part of the long
+// groups and of the short ones.  L.blocks and more: none.
+__device__ __forceinline__ uint32_t chunk_tile(const Launch& L) {
+  const uint32_t j = blockIdx.x >> 3, chunk = j / L.chunk;
+  return (chunk * 8 + (blockIdx.x & 7)) * L.chunk + (j - chunk * L.chunk);
 }
 
 // y and dx: one slot of a group's rows, one tile of the output's columns
@@ -105,12 +113,12 @@ template <int TYPE, int WHICH, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void group_rows_kernel(GroupArgs g, Launch L) {
   typedef tile::Tile<TYPE, KC, WHICH == GP_FORWARD ? KC : KR, BM, BN, WM, WN> Tl;
   constexpr int ES = TYPE == OT_F32 ? 4 : 2;
-  constexpr int BAND = BM >= 256 ? 4 : 8;
   __shared__ __attribute__((aligned(1024))) char lds0[Tl::STAGE], lds1[Tl::STAGE];
   // Few rows a matrix: little is shared, and the XCDs are kept even by taking the tiles in turn.
-  const uint32_t at = BM >= 128 ? tile::xcd_place(blockIdx.x, L.blocks) : blockIdx.x;
+  const uint32_t at = BM >= 128 ? chunk_tile(L) : blockIdx.x;
+  if (at >= L.blocks) return;
   uint32_t slot, col;
-  band_tile<BAND>(at, L.row_tiles, L.col_tiles, slot, col);
+  band_tile(at, L.band, L.row_tiles, L.col_tiles, slot, col);
   const int j0 = (int)col * BN;
   int4 at_slot;
   if (!find_slot(g, L, L.first + slot, false, at_slot)) return;
@@ -134,11 +142,8 @@ __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Lau
   typedef tile::Tile<TYPE, KR, KR, BM, BN, WM, WN> Tl;
   constexpr int ES = TYPE == OT_F32 ? 4 : 2;
   __shared__ __attribute__((aligned(1024))) char lds0[Tl::STAGE], lds1[Tl::STAGE];
-  // The tiles of a slot in chunks, which the XCDs take in turn: one XCD's workgroups share operands, and every XCD gets
-  // a part of each long slot.
   const int tiles = L.row_tiles * L.col_tiles;
-  const uint32_t j = blockIdx.x >> 3, chunk = j / L.chunk;
-  const uint32_t at = (chunk * 8 + (blockIdx.x & 7)) * L.chunk + (j - chunk * L.chunk);
+  const uint32_t at = chunk_tile(L);
   if (at >= L.blocks) return;
   int4 slot;
   if (!find_slot(g, L, L.first + at / tiles, true, slot)) return;
@@ -255,16 +260,26 @@ int64_t tiles_of(int64_t v, int b) { return (v + b - 1) / b; }
 // a launch takes so many workgroups; of more, the slots are launched in turn
 constexpr int64_t kLaunch = 1 << 22;
 
+// workgroups such that chunk_tile() gives every tile
+unsigned chunk_grid(const Launch& L) { return (unsigned)(tiles_of(L.blocks, 8 * (int)L.chunk) * 8 * L.chunk); }
+
 template <int TYPE, int WHICH, int BM, int BN, int WM, int WN>
 void launch_rows(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) {
   L.slots = p.rows.at;
   L.shift = p.rows.shift;
   L.col_tiles = (int)tiles_of(WHICH == GP_FORWARD ? g.m : g.k, BN);
+  // A chunk is a band.  (XCDs with an eighth of all tiles in a row each: float16, one group of 32,768 rows, 2,048 to 4,096,
+  // y 540 us for 501, dx 582 for 484; 1,024 groups, 65,536 rows, 512 to 1,024: 306 and 272 for 281 and 259.  Bands of two
+  // keep the XCDs even where there are few slots: 8 groups of 1,024 rows, 2,048 x 2,048: 112 for 102; float32, 8 of 2,048,
+  // 1,024 to 2,048: 598 for 545.)
+  L.band = BM < 128 ? 8 : p.rows.count >= 160 ? 4 : 2;
+  L.chunk = L.band * L.col_tiles;
   const int64_t step = kLaunch / L.col_tiles;   // col_tiles <= 1024
   for (L.first = 0; L.first < p.rows.count; L.first += step) {
     L.row_tiles = (int)std::min(step, p.rows.count - L.first);
     L.blocks = (uint32_t)L.row_tiles * L.col_tiles;
-    group_rows_kernel<TYPE, WHICH, BM, BN, WM, WN><<<L.blocks, 64 * WM * WN, 0, s>>>(g, L);
+    const unsigned grid = BM >= 128 ? chunk_grid(L) : L.blocks;
+    group_rows_kernel<TYPE, WHICH, BM, BN, WM, WN><<<grid, 64 * WM * WN, 0, s>>>(g, L);
   }
 }
 
@@ -283,9 +298,8 @@ void launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) 
     // bfloat16, 32 groups, 65,536 rows, the longest group 3 times the average, 2,048 x 2,048: 817 us for 566; float32,
     // 1,345 groups, 40,000 rows, sizes as 1 / rank, 400 x 400: 860 for 500.)
     L.chunk = (uint32_t)(tiles >= 64 ? tiles / 8 : tiles);
-    const unsigned grid = (unsigned)(tiles_of(L.blocks, 8 * (int)L.chunk) * 8 * L.chunk);
     constexpr int WN = B == 256 ? 4 : 2;
-    group_da_kernel<TYPE, B, B, 2, WN><<<grid, 128 * WN, 0, s>>>(g, L);
+    group_da_kernel<TYPE, B, B, 2, WN><<<chunk_grid(L), 128 * WN, 0, s>>>(g, L);
   }
   if (p.joins > 0) {
     // most entries are groups of one slot, whose workgroups end at once: 16,384 in all

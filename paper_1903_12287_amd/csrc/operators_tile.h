@@ -393,11 +393,4 @@ struct Tile {
   }
 };
 
-// Hardware hands workgroups to the eight XCDs in turn, each with an L2 of its own: the workgroup's place such that
-// every XCD takes one run of consecutive places.
-__device__ __forceinline__ uint32_t xcd_place(uint32_t id, uint32_t n) {
-  const uint32_t q = n >> 3, r = n & 7, xcd = id & 7;
-  return xcd * q + min(xcd, r) + (id >> 3);
-}
-
 }  // namespace tile
