@@ -18,8 +18,8 @@
  * Matrices of rows take a row stride (ld, in elements) of at least their width and at most PBG_OPS_MAX_LD; columns are
  * consecutive.  Element pointers must be aligned to their element, nothing more; rows that start at multiples of 16
  * bytes are read fastest (pbg_group_linear first copies operands whose rows do not into the workspace, which grows to
- * hold them).  Arrays lie on the context's device.  An output may not overlap an input or another output unless stated (INVALID_ARG; two
- * matrices with the same row stride and type may share rows' memory in columns of their own).
+ * hold them).  Arrays lie on the context's device.  An output may not overlap an input or another output unless
+ * stated (INVALID_ARG; two matrices with the same row stride and type may share rows' memory in columns of their own).
  */
 #ifndef PBG_OPERATORS_H
 #define PBG_OPERATORS_H
@@ -70,9 +70,9 @@ pbg_status pbg_group_linear_backward(pbg_ctx* ctx, int32_t dtype, const void* x,
  *               every score is -inf; left as it is for rows outside every sequence
  * ref_logp [2 pairs] float32 (the frozen model's logp; NULL: zeros); loss [pairs], logp, dlogp [2 pairs] and
  * row_stats [n x 2] are float32; loss and dlogp may be NULL (a frozen model's pass).  Infinities and NaN in scores that
- * count reach the results by the formulas.  offsets [2 pairs + 1] int64 as in pbg_group_linear; beta finite, smoothing in [0, 1);
- * candidates <= PBG_OPS_MAX_LD; pairs in [1, PBG_OPS_MAX_GROUPS / 2]; n < 2^24 - 1.  INVALID_ARG for bad offsets and for a label of a row inside a sequence
- * that is >= candidates. */
+ * count reach the results by the formulas.  offsets [2 pairs + 1] int64 as in pbg_group_linear; beta finite,
+ * smoothing in [0, 1); candidates <= PBG_OPS_MAX_LD; pairs in [1, PBG_OPS_MAX_GROUPS / 2]; n < 2^24.  INVALID_ARG for
+ * bad offsets and for a label of a row inside a sequence that is >= candidates. */
 pbg_status pbg_preference_loss(pbg_ctx* ctx, int32_t dtype, const void* logits, int64_t ld, const int32_t* labels,
                                const int64_t* offsets, int32_t pairs, int64_t n, int32_t candidates,
                                const float* ref_logp, float beta, float smoothing, float* loss, float* logp,
@@ -90,7 +90,8 @@ pbg_status pbg_preference_loss_backward(pbg_ctx* ctx, int32_t dtype, const void*
 
 /* The joint norm of num_tensors gradients, sqrt(sum of all squares), and their scaling to at most max_norm:
  *   outs[i] = grads[i] * min(1, max_norm / norm)
- * dtypes_host [num_tensors] int32 (PBG_TYPE_*), counts_host [num_tensors] int64 (elements, at most 2^38 together; 0 is allowed, with NULL pointers),
+ * dtypes_host [num_tensors] int32 (PBG_TYPE_*), counts_host [num_tensors] int64 (elements, at most 2^38 together; 0
+ * is allowed, with NULL pointers),
  * grads_host and outs_host [num_tensors] host arrays of device pointers to contiguous values.  outs_host NULL, or
  * outs_host[i] equal to grads_host[i]: in place.  No output may overlap another tensor (INVALID_ARG).  max_norm > 0;
  * +inf: only the norm (in place nothing is written).  norm_host (nullable) receives the norm.  Squares are summed in

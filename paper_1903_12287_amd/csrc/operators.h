@@ -54,7 +54,8 @@ struct GroupPlan {
 GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int64_t k, bool want_da);
 // the tables of slots, and offsets[0..groups] nondecreasing and within [0, n], else OPS_BAD_OFFSETS into *flag (nothing
 // where there are no tables)
-void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, int64_t n, uint32_t* flag, hipStream_t s);
+void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, int64_t n, uint32_t* flag,
+                       hipStream_t s);
 // up to three operands into rows of wp values, a multiple of 16 bytes, zeros behind `width`
 void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,
                        const int64_t* rows, const int* width, const int* wp, hipStream_t s);

@@ -2,11 +2,15 @@
 // norm = sqrt(sum of all squares), out = g min(1, max_norm / norm).
 //
 // Bound by memory: the gradients are read for the norm, read again and written.  A workgroup takes 8,192 values of one
-// tensor at a time, 16 bytes a load, all of a thread's loads on their way at once; its sum of squares goes to a place of its
-// own, so the norm does not depend on the order in which workgroups end.  The scaling walks the workgroups backwards:
-// what the norm read last is still in the 256 MB cache beside the memory.  Squares and their sums are float64
-// (an instruction a value: the vector unit keeps up with memory), so the norm neither overflows nor loses small
+// tensor at a time, 16 bytes a load, all of a thread's loads on their way at once; its sum of squares goes to a place of
+// its own, so the norm does not depend on the order in which workgroups end.  The scaling walks the workgroups
+// backwards: what the norm read last is still in the 256 MB cache beside the memory.  Squares and their sums are
+// float64 (an instruction a value: the vector unit keeps up with memory), so the norm neither overflows nor loses small
 // gradients, and a scaled value is rounded once, to its own type.
+//
+// Measured: 620 million float32 values (2.48 GB) 418 us for the squares (5.9 TB/s) and 907 for the scaling (5.5 TB/s
+// read and written; a large copy reaches 5.1); 59 tensors of 50 million values of two types 22 and 41 us, the second
+// read mostly from the cache, 5 for the factor between them and 17 for 59 descriptors, launches and the wait.
 #include "operators_device.h"
 
 namespace {

@@ -7,6 +7,17 @@
 // workgroup searching the offsets itself: four loads one behind the other before its first fetch, 2.5 of the 10 us of
 // a workgroup with 32 rows of 400.)  Offsets of up to 63 groups fit the lanes of a wave: there every wave reads and
 // checks them all in one load, and small products need no kernel ahead of them.
+//
+// Measured and what bounds it (us; the product alone, without the call's 15):
+//   float32, 1,345 groups, 40,000 rows, 400 x 400, y: 261.  989 MB at 4.3 TB/s of 5.1 that a copy reaches; 52 TFLOP/s.
+//   bfloat16, 32 groups, 32,768 rows, 2,048 to 4,096, y: 560, 980 TFLOP/s; one group: 500, 1,100.  A large library
+//     product reaches 1,370.  The slices' way from memory bounds it: the loads alone, nothing multiplied, take as long
+//     (585; 389 where all operands lie in the cache beside the memory), while LDS reads are hidden and products alone
+//     take 425.  Two slices of 64 KB are what the LDS holds, and a slice waits for its slowest row.  What did not help:
+//     reading ahead into the L2 (4 or 16 bytes a line, a slice or four ahead), padded rows, a persistent workgroup
+//     that fetches the next tile's slices before it stores (1 to 5 %).
+//   bfloat16, 32 groups, 16,384 rows, 2,048 x 2,048: dx 195 (705 TFLOP/s), da 245 (560; 268 MB written).
+//   float16, 24 rows in 16 groups, 2,048 x 2,048, y: 18, 134 MB of matrices read at 7.5 TB/s (partly from the cache).
 #include <algorithm>
 
 #include "operators_tile.h"
@@ -101,8 +112,8 @@ __device__ __forceinline__ void band_tile(uint32_t at, uint32_t band, uint32_t s
 }
 
 // Hardware hands workgroups to the eight XCDs in turn, each with an L2 of its own: the tile of this workgroup such that
-// the XCDs take chunks of L.chunk tiles in turn.  Tiles in a chunk share operands; and every XCD gets its part of the long
-// groups and of the short ones.  L.blocks and more: none.
+// the XCDs take chunks of L.chunk tiles in turn.  Tiles in a chunk share operands; and every XCD gets its part of the
+// long groups and of the short ones.  L.blocks and more: none.
 __device__ __forceinline__ uint32_t chunk_tile(const Launch& L) {
   const uint32_t j = blockIdx.x >> 3, chunk = j / L.chunk;
   return (chunk * 8 + (blockIdx.x & 7)) * L.chunk + (j - chunk * L.chunk);
@@ -129,9 +140,11 @@ __global__ __launch_bounds__(64 * WM * WN) void group_rows_kernel(GroupArgs g, L
   v4f acc[Tl::IB][Tl::JB];
   const int width = WHICH == GP_FORWARD ? g.m : g.k;
   if (WHICH == GP_FORWARD)
-    Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.x + r0 * g.ldx * ES, g.ldx, rows, a + (int64_t)j0 * g.lda * ES, g.lda, g.m - j0, g.kd, acc);
+    Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.x + r0 * g.ldx * ES, g.ldx, rows,
+            a + (int64_t)j0 * g.lda * ES, g.lda, g.m - j0, g.kd, acc);
   else
-    Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.dy + r0 * g.lddy * ES, g.lddy, rows, a + (int64_t)j0 * ES, g.lda, g.kd - j0, g.m, acc);
+    Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.dy + r0 * g.lddy * ES, g.lddy, rows,
+            a + (int64_t)j0 * ES, g.lda, g.kd - j0, g.m, acc);
   Tl::template store<TYPE>(acc, (char*)g.out + (r0 * g.ldo + j0) * ES, g.ldo, rows, width - j0);
 }
 
@@ -153,8 +166,8 @@ __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Lau
   const int64_t r0 = slot.x, depth = slot.y;
   const int grp = slot.z;
   v4f acc[Tl::IB][Tl::JB];
-  Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.dy + (r0 * g.lddy + i0) * ES, g.lddy, g.md - i0, (const char*)g.x + (r0 * g.ldx + j0) * ES,
-          g.ldx, g.kd - j0, depth, acc);
+  Tl::run((tile::lds_t*)lds0, (tile::lds_t*)lds1, (const char*)g.dy + (r0 * g.lddy + i0) * ES, g.lddy, g.md - i0,
+          (const char*)g.x + (r0 * g.ldx + j0) * ES, g.ldx, g.kd - j0, depth, acc);
   const int rows = min(BM, g.m - i0), cols = g.k - j0;
   if (slot.w < 0) {
     Tl::template store<TYPE>(acc, (char*)g.out + (((int64_t)grp * g.m + i0) * g.k + j0) * ES, g.k, rows, cols);
@@ -165,8 +178,8 @@ __global__ __launch_bounds__(64 * WM * WN) void group_da_kernel(GroupArgs g, Lau
 }
 
 // Adds a group's partial sums: of more than 32, 64 elements a workgroup, each of its four waves a quarter of the slots
-// in their order, then the waves in theirs.  (One thread an element over all slots: 65 us for 78 slots of 100 x 100, loads one behind
-// the other.)
+// in their order, then the waves in theirs.  (One thread an element over all slots: 65 us for 78 slots of 100 x 100,
+// loads one behind the other; 4 us so.)
 template <int TYPE>
 __global__ __launch_bounds__(256) void group_join_kernel(GroupArgs g, Launch L) {
   typedef typename Elem<TYPE>::T T;
@@ -268,10 +281,10 @@ void launch_rows(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s
   L.slots = p.rows.at;
   L.shift = p.rows.shift;
   L.col_tiles = (int)tiles_of(WHICH == GP_FORWARD ? g.m : g.k, BN);
-  // A chunk is a band.  (XCDs with an eighth of all tiles in a row each: float16, one group of 32,768 rows, 2,048 to 4,096,
-  // y 540 us for 501, dx 582 for 484; 1,024 groups, 65,536 rows, 512 to 1,024: 306 and 272 for 281 and 259.  Bands of two
-  // keep the XCDs even where there are few slots: 8 groups of 1,024 rows, 2,048 x 2,048: 112 for 102; float32, 8 of 2,048,
-  // 1,024 to 2,048: 598 for 545.)
+  // A chunk is a band.  (XCDs with an eighth of all tiles in a row each: float16, one group of 32,768 rows, 2,048 to
+  // 4,096, y 540 us for 501, dx 582 for 484; 1,024 groups, 65,536 rows, 512 to 1,024: 306 and 272 for 281 and 259.
+  // Bands of two keep the XCDs even where there are few slots: 8 groups of 1,024 rows, 2,048 x 2,048: 112 for 102;
+  // float32, 8 of 2,048, 1,024 to 2,048: 598 for 545.)
   L.band = BM < 128 ? 8 : p.rows.count >= 160 ? 4 : 2;
   L.chunk = L.band * L.col_tiles;
   const int64_t step = kLaunch / L.col_tiles;   // col_tiles <= 1024
@@ -309,10 +322,11 @@ void launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) 
   }
 }
 
-// Rows and columns of a tile of da: in float32 the matrix unit sets the time, and more, smaller workgroups keep it busier
-// (8 groups, 40,000 rows, 100 x 100: both gradients 70 us for 75); in 16 bits reading the operands does (128 x 128 / 256 x
-// 256, of 2,048 x 2,048: 32 groups of 512 rows 267 / 248 us, of 2,048 rows 610 / 535, uneven ones 672 / 566; where
-// groups have to be cut to give every compute unit a tile, 4 groups of 4,096 rows: 153 / 258).
+// Rows and columns of a tile of da: in float32 the matrix unit sets the time, and more, smaller workgroups keep it
+// busier (8 groups, 40,000 rows, 100 x 100: both gradients 75 us by 128 x 128, 70 by 64 x 64); in 16 bits reading the
+// operands does (128 x 128 / 256 x 256, of 2,048 x 2,048: 32 groups of 512 rows 267 / 248 us, of 2,048 rows 610 / 535,
+// uneven ones 672 / 566; where groups have to be cut to give every compute unit a tile, 4 groups of 4,096 rows:
+// 153 / 258).
 int da_tile(int type, int64_t n, int64_t groups, int64_t m, int64_t k) {
   if (type == OT_F32) return 64;
   return n / groups >= 512 && groups * tiles_of(m, 256) * tiles_of(k, 256) >= 512 ? 256 : 128;
@@ -415,10 +429,12 @@ __global__ __launch_bounds__(256) void group_plan_kernel(GroupPlan p, const int6
 
 }  // namespace
 
-void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, int64_t n, uint32_t* flag, hipStream_t s) {
+void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, int64_t n, uint32_t* flag,
+                       hipStream_t s) {
   if (!p.tables) return;
   const int64_t work = std::max<int64_t>(p.rows.count + p.da.count + p.joins, groups + 1);
-  group_plan_kernel<<<(unsigned)std::min<int64_t>(tiles_of(work, 256), 65536), 256, 0, s>>>(p, offsets, groups, n, flag);
+  const unsigned blocks = (unsigned)std::min<int64_t>(tiles_of(work, 256), 65536);
+  group_plan_kernel<<<blocks, 256, 0, s>>>(p, offsets, groups, n, flag);
 }
 
 GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int64_t k, bool want_da) {
@@ -432,7 +448,10 @@ GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int6
   }
   if (!want_da) return p;
   // Rows of a slot of da: enough slots for a few workgroups on each of the 256 compute units, where the matrices' tiles
-  // alone are not; with tiles enough, only groups of four times the average and more are cut.
+  // alone are not, but 256 rows (of 128: float16, 37 groups of 135 rows, 336 x 504: 59 us for 33, partial sums written
+  // and read); with tiles enough, longer groups than four times the average in 16 bits (twice: 32 groups, 16,384 rows,
+  // 2,048 x 2,048: 288 for 259), than the average in float32 (four times: 37 groups, 5,000 rows, sizes as 1 / rank^1.5,
+  // 336 x 504: 106 for 71).
   p.da_tile = da_tile(type, n, groups, m, k);
   const int64_t tiles = tiles_of(m, p.da_tile) * tiles_of(k, p.da_tile);
   int64_t rows = std::max<int64_t>(256, n * tiles / 1024);

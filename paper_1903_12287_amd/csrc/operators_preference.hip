@@ -9,6 +9,10 @@
 // Bound by memory: the scores are read for the loss, read again and overwritten by the gradient.  Rows without a label
 // are not read.  16 bytes a load wherever the row starts; a wave takes a row of up to 2,048 candidates, a workgroup a
 // longer one, and few rows are cut into segments whose (m, sum) are joined afterwards.
+//
+// Measured, bfloat16, 16,384 rows of 15,000 candidates, a fifth of them without a label: 111 us for the sums (393 MB,
+// 3.5 TB/s: an exponential a score keeps the vector unit as busy as the memory), 155 for the gradient (393 MB read, 492
+// written, 5.7 TB/s; a large copy reaches 5.1).  float16, 96 rows of 131,001: 10 us for the parts, 8 to join them.
 #include <algorithm>
 
 #include "operators_device.h"
@@ -371,8 +375,8 @@ void launch_loss_typed(const PrefArgs& p, hipStream_t s) {
   pair_loss_kernel<TYPE, false><<<p.pairs, p.n / p.pairs > 8192 ? 1024 : 256, 0, s>>>(p);
 }
 
-// Up to so many rows and sequences every workgroup of the gradient checks them all, a few loads a thread, which saves the
-// launch of a kernel ahead of it (2.5 of a small call's 20 us).
+// Up to so many rows and sequences every workgroup of the gradient checks them all, a few loads a thread, which saves
+// the launch of a kernel ahead of it (2.5 of a small call's 20 us).
 constexpr int64_t kCheckHere = 512;
 
 template <int TYPE, bool WAVE>

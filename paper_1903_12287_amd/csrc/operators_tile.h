@@ -187,8 +187,9 @@ struct Tile {
 
   // acc[i][j][r]: row 16 i + lane % 16, column 16 j + 4 (lane / 16) + r of the wave's part (Q feeds the matrix
   // instruction's rows, so that a lane holds four consecutive columns of C)
-  __device__ __forceinline__ static void run(lds_t* lds0, lds_t* lds1, const void* p, int64_t ldp, int rows, const void* q, int64_t ldq,
-                                             int cols, int64_t depth, v4f (&acc)[IB][JB]) {
+  __device__ __forceinline__ static void run(lds_t* lds0, lds_t* lds1, const void* p, int64_t ldp, int rows,
+                                             const void* q, int64_t ldq, int cols, int64_t depth,
+                                             v4f (&acc)[IB][JB]) {
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = w / WN, wn = w % WN;
     P op;
@@ -237,10 +238,10 @@ struct Tile {
     oq.fetch(stage, P::BYTES, kt);
   }
 
-  // The products by eight waves, two on each of the four units, which take turns: one reads half a slice while the other
-  // multiplies its half; a slice is four turns, the second wave a turn behind.  Half as many registers hold what was
-  // read, which two KR operands at 256 x 256 need.  (Where both fit, slices() is faster by 0 to 5 %: a fetch has a slice
-  // and a half to arrive there, one here.)  IA 0: the wave only moves its share.
+  // The products by eight waves, two on each of the four units, which take turns: one reads half a slice while the
+  // other multiplies its half; a slice is four turns, the second wave a turn behind.  Half as many registers hold what
+  // was read, which two KR operands at 256 x 256 need.  (Where both fit, slices() is faster by 0 to 5 %: a fetch has a
+  // slice and a half to arrive there, one here.)  IA 0: the wave only moves its share.
   template <int IA>
   __device__ __forceinline__ static void turns(lds_t* lds0, lds_t* lds1, const P& op, const Q& oq, int nk, bool second,
                                                v4f (&acc)[IB][JB]) {
