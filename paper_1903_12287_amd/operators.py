@@ -7,6 +7,7 @@ pointers and raises pbg.PbgError when the call returns an error status.  Context
 
 from __future__ import annotations
 
+import array
 import ctypes
 
 import torch
@@ -95,14 +96,16 @@ def _here(*tensors):
 
 
 def _values(tensors, what):
-    """Types, numbers of values and pointers of contiguous device tensors of any shapes (an attribute at a time over
-    all of them: half the time of a loop over tensors)."""
+    """Types, numbers of values and pointers of contiguous device tensors of any shapes, as arrays (an attribute at a
+    time over all of them: half the time of a loop over tensors; arrays, not ctypes': a quarter of theirs)."""
+    T = torch.Tensor
     try:
         types = [TYPES[t.dtype] for t in tensors]
-        d = {t.get_device() for t in tensors}   # -1: the host
-        if (not d or d == {torch.cuda.current_device()}) and all([t.is_contiguous() for t in tensors]):
-            return types, [t.numel() for t in tensors], [t.data_ptr() for t in tensors]
-    except (KeyError, AttributeError, RuntimeError):   # the last: no device at all
+        d = set(map(T.get_device, tensors))   # -1: the host
+        if (not d or d == {torch.cuda.current_device()}) and all(map(T.is_contiguous, tensors)):
+            return (array.array("i", types), array.array("q", list(map(T.numel, tensors))),
+                    array.array("Q", list(map(T.data_ptr, tensors))))
+    except (KeyError, AttributeError, TypeError, RuntimeError):   # the last: no device at all
         pass
     for i, t in enumerate(tensors):   # which one, and why
         pbg._ptr(t, _type(t, f"{what}[{i}]"), f"{what}[{i}]")
@@ -191,8 +194,8 @@ def pbg_preference_loss_backward(ctx, logits, labels, offsets, row_stats, dlogp,
 
 
 def pbg_clip_gradients(ctx, grads, max_norm, outs=None) -> float:
-    """grads: tensors of any shapes (contiguous; float32, bfloat16, float16 mixed); outs: as many tensors of their types and
-    sizes, or None to scale in place.  Returns the joint norm before the scaling."""
+    """grads: tensors of any shapes (contiguous; float32, bfloat16, float16 mixed); outs: as many tensors of their types
+    and sizes, or None to scale in place.  Returns the joint norm before the scaling."""
     n = len(grads)
     if outs is not None and len(outs) != n:
         raise ValueError("one output per gradient")
@@ -202,9 +205,8 @@ def pbg_clip_gradients(ctx, grads, max_norm, outs=None) -> float:
         otypes, ocounts, op = _values(outs, "outs")
         if otypes != types or ocounts != counts:
             raise ValueError("every output must have its gradient's type and number of values")
-    m = max(n, 1)
-    types, counts = (ctypes.c_int32 * m)(*types), (ctypes.c_int64 * m)(*counts)
-    gp, op = (ctypes.c_void_p * m)(*gp), None if op is None else (ctypes.c_void_p * m)(*op)
+    at = lambda v: None if v is None else v.buffer_info()[0]   # the arrays live until the call has returned
     norm = ctypes.c_double(0.0)
-    _check(ctx, library().pbg_clip_gradients(ctx, n, types, counts, gp, op, float(max_norm), ctypes.byref(norm)))
+    _check(ctx, library().pbg_clip_gradients(ctx, n, at(types), at(counts), at(gp), at(op), float(max_norm),
+                                             ctypes.byref(norm)))
     return norm.value
