@@ -7,12 +7,12 @@
 // zero the scores lie.
 //
 // Bound by memory: the scores are read for the loss, read again and overwritten by the gradient.  Rows without a label
-// are not read.  16 bytes a load wherever the row starts; a wave takes a row of up to 2,048 candidates, a workgroup a
-// longer one, and few rows are cut into segments whose (m, sum) are joined afterwards.
+// are not read.  16 bytes a load wherever the row starts; a wave takes a short row, a workgroup a longer one, and few rows
+// are cut into segments whose (m, sum) are joined afterwards.
 //
-// Measured, bfloat16, 16,384 rows of 15,000 candidates, a fifth of them without a label: 111 us for the sums (393 MB,
-// 3.5 TB/s: an exponential a score keeps the vector unit as busy as the memory), 155 for the gradient (393 MB read, 492
-// written, 5.7 TB/s; a large copy reaches 5.1).  float16, 96 rows of 131,001: 10 us for the parts, 8 to join them.
+// Measured, bfloat16, 16,384 rows of 15,000 candidates, a fifth of them without a label: 75 us for the sums (393 MB, 5.2
+// TB/s; an exponential a score), 155 for the gradient (393 MB read, 492 written, 5.7 TB/s; a large copy reaches 5.1).
+// float16, 96 rows of 131,001: 9 us for the parts, 8 to join them.
 #include <algorithm>
 
 #include "operators_device.h"
@@ -359,8 +359,12 @@ void check(const PrefArgs& p, hipStream_t s) {
   check_preference_kernel<<<(unsigned)std::min<int64_t>((work + 255) / 256, 1024), 256, 0, s>>>(p);
 }
 
-// a wave takes a row of up to so many candidates: 32 loads a lane at most
-constexpr int kWaveRow = 2048;
+// A wave takes a row of up to so many bytes, a workgroup a longer one: a workgroup's start and end are spread over four
+// rows, a long row's own work over four waves.  Loss, us, wave / workgroup: bfloat16, 65,536 rows of 2,500 89 / 158,
+// 20,000 of 7,000 62 / 67, 8,192 of 12,000 52 / 53, 16,384 of 15,000 99 / 93; float32, 16,384 of 5,000 66 / 79, of 8,000
+// 103 / 98.  Gradient: bfloat16, 65,536 rows of 2,500 155 / 196, 40,000 of 4,096 134 / 136, 32,768 of 5,000 147 / 138;
+// float32, 40,000 of 2,500 172 / 160.
+constexpr int kWaveStats = 24576, kWaveGradient = 8192;
 
 template <int TYPE>
 void launch_loss_typed(const PrefArgs& p, hipStream_t s) {
@@ -370,7 +374,7 @@ void launch_loss_typed(const PrefArgs& p, hipStream_t s) {
     return;
   }
   check(p, s);
-  if (p.V <= kWaveRow) row_stats_kernel<TYPE, true><<<(unsigned)((p.n + 3) / 4), 256, 0, s>>>(p);
+  if (p.V * (int)sizeof(typename Elem<TYPE>::T) <= kWaveStats) row_stats_kernel<TYPE, true><<<(unsigned)((p.n + 3) / 4), 256, 0, s>>>(p);
   else row_stats_kernel<TYPE, false><<<(unsigned)p.n, 256, 0, s>>>(p);
   pair_loss_kernel<TYPE, false><<<p.pairs, p.n / p.pairs > 8192 ? 1024 : 256, 0, s>>>(p);
 }
@@ -392,7 +396,7 @@ void launch_gradient(const PrefArgs& p, int64_t blocks, hipStream_t s) {
 template <int TYPE>
 void launch_backward_typed(PrefArgs p, hipStream_t s) {
   const int64_t rows = std::max<int64_t>(p.n, 1);
-  if (p.V <= kWaveRow) {
+  if (p.V * (int)sizeof(typename Elem<TYPE>::T) <= kWaveGradient) {
     launch_gradient<TYPE, true>(p, (rows + 3) / 4, s);
   } else {
     // four workgroups and more on each of the 256 compute units where there are few rows
