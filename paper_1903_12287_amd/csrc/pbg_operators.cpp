@@ -1,6 +1,7 @@
 // Host side of the operators on a caller's own tensors (include/pbg_operators.h): argument checks, workspace and
 // launch sequence.  A call checks on the host what the host can see; what lies in device arrays (offsets, labels) is
-// checked by a kernel ahead of the work, whose verdict every workgroup behind it reads before it writes anything.
+// checked by a kernel ahead of the work, whose word every workgroup behind it reads before it writes anything, or, where
+// there is little of it, by every workgroup itself.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -205,3 +205,48 @@ def test_gradients_of_large_matrices(ctx, sizes, k, m, t):
         r = slice(int(off[g]), int(off[g + 1]))
         exact = dy[r].float().t().contiguous() @ x[r].float()
         assert torch.equal(da[g], exact.to(t))
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.float16])
+@pytest.mark.parametrize("n,k,m", [(300, 64, 72), (300, 50, 33), (40, 1, 1)])
+def test_largest_row_stride(ctx, t, n, k, m):
+    ld = 1 << 20
+    x, dy, a = small_integers(10, n, k, dtype=t), small_integers(11, n, m, dtype=t), small_integers(12, 2, m, k, dtype=t)
+    off = offsets(0, n // 3, n)
+
+    def wide(v=None, width=None):
+        w = torch.full((n, ld), 9.0, dtype=t, device="cuda")[:, 5:5 + (width or v.shape[1])]
+        if v is not None:
+            w.copy_(v)
+        return w
+
+    y, dx = wide(width=m), wide(width=k)
+    da = torch.empty(2, m, k, dtype=t, device="cuda")
+    ops.pbg_group_linear(ctx, wide(x), a, off, y)
+    ops.pbg_group_linear_backward(ctx, wide(x), a, off, wide(dy), dx, da)
+    y2, dx2, da2 = torch.empty_like(dy), torch.empty_like(x), torch.empty_like(da)
+    ops.pbg_group_linear(ctx, x, a, off, y2)
+    ops.pbg_group_linear_backward(ctx, x, a, off, dy, dx2, da2)
+    assert torch.equal(y, y2) and torch.equal(dx, dx2) and torch.equal(da, da2)
+    for g, r in ((0, slice(0, n // 3)), (1, slice(n // 3, n))):
+        assert torch.equal(y2[r], (x[r].double() @ a[g].double().t()).to(t))
+        assert torch.equal(dx2[r], (dy[r].double() @ a[g].double()).to(t))
+        assert torch.equal(da2[g], (dy[r].double().t() @ x[r].double()).to(t))
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+def test_largest_number_of_groups(ctx, t):
+    G, n, k, m = 1 << 20, 3000, 4, 8
+    rows = np.sort(np.random.default_rng(0).integers(0, G, n))   # most groups are empty
+    off = torch.from_numpy(np.searchsorted(rows, np.arange(G + 1)).astype(np.int64)).cuda()
+    group = torch.from_numpy(rows).cuda()
+    x, dy, a = small_integers(13, n, k, dtype=t), small_integers(14, n, m, dtype=t), small_integers(15, G, m, k, dtype=t)
+    y, dx, da = torch.empty_like(dy), torch.empty_like(x), torch.full_like(a, 9)
+    ops.pbg_group_linear(ctx, x, a, off, y)
+    ops.pbg_group_linear_backward(ctx, x, a, off, dy, dx, da)
+    mine = a[group].double()
+    assert torch.equal(y.double(), (mine * x.double()[:, None, :]).sum(2))
+    assert torch.equal(dx.double(), (mine * dy.double()[:, :, None]).sum(1))
+    want = torch.zeros(G, m, k, dtype=torch.float64, device="cuda")
+    want.index_add_(0, group, dy.double()[:, :, None] * x.double()[:, None, :])
+    assert torch.equal(da.double(), want)
