@@ -17,9 +17,10 @@
  *
  * Matrices of rows take a row stride (ld, in elements) of at least their width and at most PBG_OPS_MAX_LD; columns are
  * consecutive.  Element pointers must be aligned to their element, nothing more; rows that start at multiples of 16
- * bytes are read fastest (pbg_group_linear first copies operands whose rows do not into the workspace, which grows to
- * hold them).  Arrays lie on the context's device.  An output may not overlap an input or another output unless
- * stated (INVALID_ARG; two matrices with the same row stride and type may share rows' memory in columns of their own).
+ * bytes are read fastest (the grouped products first copy operands whose rows do not into the workspace, which grows to
+ * hold them: of the groups' matrices only those of groups that have rows, and no more than there are rows).  Arrays
+ * lie on the context's device.  An output may not overlap an input or another output unless stated (INVALID_ARG; two
+ * matrices with the same row stride and type may share rows' memory in columns of their own).
  */
 #ifndef PBG_OPERATORS_H
 #define PBG_OPERATORS_H

@@ -27,6 +27,7 @@ struct GroupArgs {
   int64_t n;
   int k, m;             // in_dim, out_dim
   int kd, md;           // widths that the operands hold: rounded up to 16 bytes where they were packed, zeros behind
+  bool a_by_row;        // a is packed with a group's matrix at place offsets[group], not at place group
   const uint32_t* bad;  // the check's verdict, read by every workgroup
   uint32_t* host_bad;   // receives it where it is not 0
 };
@@ -56,9 +57,18 @@ GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int6
 // where there are no tables)
 void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, int64_t n, uint32_t* flag,
                        hipStream_t s);
-// up to three operands into rows of wp values, a multiple of 16 bytes, zeros behind `width`
-void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,
-                       const int64_t* rows, const int* width, const int* wp, hipStream_t s);
+// An operand to be packed: rows of `wp` values, a multiple of 16 bytes, with zeros behind `width`.  Rows that no group
+// holds are left out.
+struct GroupPack {
+  const void* src;
+  void* dst;
+  int64_t ld;           // of src; dst's rows are wp apart
+  int64_t rows;         // of dst
+  int matrix;           // rows of a group's matrix, one matrix a place; 0: rows of x or dy
+  int width, wp;
+};
+// up to three of them
+void launch_group_pack(int type, int count, const GroupPack* op, const int64_t* offsets, int groups, hipStream_t s);
 void launch_group_product(const GroupArgs& g, int type, int which, const GroupPlan& p, hipStream_t s);
 
 // ---- preference loss ----------------------------------------------------------------------------

@@ -136,7 +136,7 @@ __global__ __launch_bounds__(64 * WM * WN) void group_rows_kernel(GroupArgs g, L
   const int64_t r0 = at_slot.x;
   const int rows = at_slot.y, grp = at_slot.z;
   if (rows <= 0) return;
-  const char* a = (const char*)g.a + grp * g.a_group * ES;
+  const char* a = (const char*)g.a + (g.a_by_row ? g.offsets[grp] : grp) * g.a_group * ES;
   v4f acc[Tl::IB][Tl::JB];
   const int width = WHICH == GP_FORWARD ? g.m : g.k;
   if (WHICH == GP_FORWARD)
@@ -234,15 +234,27 @@ __global__ __launch_bounds__(256) void group_join_kernel(GroupArgs g, Launch L) 
   }
 }
 
-// Copies rows of `width` values into rows of `wp` >= width, a multiple of 16 bytes, with zeros behind them.
+// Copies rows of `width` values into rows of `wp` >= width, a multiple of 16 bytes, with zeros behind them.  Only what
+// the products read is copied: the rows between the first and the last offset, and the matrices of groups that have
+// rows.  Where there are fewer rows than groups, a matrix's place is its group's first row, so that the copies take no
+// more than a matrix a row, however many groups there are.  Offsets that are not in order only choose which of the
+// groups' matrices are copied to which places: they have not been checked here.
 struct PackArgs {
-  const void* src[3];
-  void* dst[3];
-  int64_t ld[3], rows[3];
-  int width[3], wp[3];
+  GroupPack op[3];
   uint32_t first[4];   // first workgroup of each
   int64_t per;         // rows of a workgroup
+  const int64_t* offsets;
+  int groups;
 };
+
+// the group whose matrix has this place (the same in all lanes of a wave), or -1: none that has rows
+__device__ __forceinline__ int group_at_place(const PackArgs& a, bool by_row, int64_t place) {
+  if (by_row) {
+    const int g = sequence_of_row(a.offsets, a.groups, place);
+    return g >= 0 && a.offsets[g] == place ? g : -1;
+  }
+  return a.offsets[place] < a.offsets[place + 1] ? (int)place : -1;
+}
 
 template <int TYPE>
 __global__ __launch_bounds__(256) void group_pack_kernel(PackArgs a) {
@@ -250,18 +262,31 @@ __global__ __launch_bounds__(256) void group_pack_kernel(PackArgs a) {
   typedef typename Vec<TYPE>::V V;
   constexpr int N = Vec<TYPE>::N;
   const int w = blockIdx.x >= a.first[2] ? 2 : (blockIdx.x >= a.first[1] ? 1 : 0);
-  const int64_t r0 = (int64_t)(blockIdx.x - a.first[w]) * a.per;
-  const int64_t r1 = min(a.rows[w], r0 + a.per);
+  const GroupPack& op = a.op[w];
+  int64_t r0 = (int64_t)(blockIdx.x - a.first[w]) * a.per, r1 = min(op.rows, r0 + a.per);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const bool by_row = op.matrix && op.rows < (int64_t)a.groups * op.matrix;
+  if (!op.matrix) {
+    r1 = min(r1, a.offsets[a.groups]);
+    r0 = max(r0, min(r1, a.offsets[0]));
+  }
+  int64_t place = -1, shift = 0;   // a matrix's rows in src lie so many behind its place's
+  int grp = 0;
   for (int64_t r = r0 + wave; r < r1; r += 4) {
-    const T* s = (const T*)a.src[w] + r * a.ld[w];
-    T* d = (T*)a.dst[w] + r * a.wp[w];
-    for (int c = lane * N; c < a.wp[w]; c += 64 * N) {   // wp is a multiple of N
-      if (c + N <= a.width[w]) {
+    if (op.matrix && (place < 0 || r >= (place + 1) * op.matrix)) {
+      place = r / op.matrix;
+      grp = group_at_place(a, by_row, place);
+      shift = (grp - place) * op.matrix;
+    }
+    if (grp < 0) continue;
+    const T* s = (const T*)op.src + (r + shift) * op.ld;
+    T* d = (T*)op.dst + r * op.wp;
+    for (int c = lane * N; c < op.wp; c += 64 * N) {   // wp is a multiple of N
+      if (c + N <= op.width) {
         *(V*)(d + c) = *(const V*)(s + c);
       } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) d[c + j] = c + j < a.width[w] ? s[c + j] : (T)0.0f;
+        for (int j = 0; j < N; ++j) d[c + j] = c + j < op.width ? s[c + j] : (T)0.0f;
       }
     }
   }
@@ -467,24 +492,20 @@ GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int6
   return p;
 }
 
-void launch_group_pack(int type, int count, const void* const* src, void* const* dst, const int64_t* ld,
-                       const int64_t* rows, const int* width, const int* wp, hipStream_t s) {
+void launch_group_pack(int type, int count, const GroupPack* op, const int64_t* offsets, int groups, hipStream_t s) {
   PackArgs a{};
+  a.offsets = offsets;
+  a.groups = groups;
   int64_t total = 0;
-  for (int i = 0; i < count; ++i) total += rows[i];
+  for (int i = 0; i < count; ++i) total += op[i].rows;
   a.per = 16;
   while (total / a.per > kLaunch) a.per *= 2;
   uint32_t at = 0;
   for (int i = 0; i < 3; ++i) {
     a.first[i] = at;
     if (i >= count) continue;
-    a.src[i] = src[i];
-    a.dst[i] = dst[i];
-    a.ld[i] = ld[i];
-    a.rows[i] = rows[i];
-    a.width[i] = width[i];
-    a.wp[i] = wp[i];
-    at += (uint32_t)((rows[i] + a.per - 1) / a.per);
+    a.op[i] = op[i];
+    at += (uint32_t)((op[i].rows + a.per - 1) / a.per);
   }
   if (!at) return;
   if (type == OT_F32) group_pack_kernel<OT_F32><<<at, 256, 0, s>>>(a);

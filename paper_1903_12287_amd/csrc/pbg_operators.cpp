@@ -95,36 +95,35 @@ bool bad_ld(int64_t ld, int64_t width) { return ld < width || ld > PBG_OPS_MAX_L
 struct Operands {
   int64_t es, ev;
   int count = 0;
-  const void* src[3];
-  void* dst[3];
-  int64_t ld[3], rows[3];
-  int width[3], wp[3];
+  GroupPack op[3];
   size_t bytes = 0;
   size_t at[3];
   const void** p[3];
   int64_t* out_ld[3];
   explicit Operands(int type) : es(type_bytes(type)), ev(16 / type_bytes(type)) {}
   int padded(int w) const { return (int)((w + ev - 1) / ev * ev); }
-  // *ptr (rows of *row_ld) is used as it is or replaced by its copy
-  void add(const void** ptr, int64_t* row_ld, int64_t n, int w) {
-    if (!*ptr || n <= 0) return;
-    if (((uintptr_t)*ptr & 15) == 0 && *row_ld % ev == 0 && w % ev == 0) return;
-    src[count] = *ptr;
-    ld[count] = *row_ld;
-    rows[count] = n;
-    width[count] = w;
-    wp[count] = padded(w);
+  // *ptr (n rows of *row_ld, `matrix` of them a matrix) is used as it is or replaced by its copy; true: copied
+  bool add(const void** ptr, int64_t* row_ld, int64_t n, int w, int matrix = 0) {
+    if (!*ptr || n <= 0) return false;
+    if (((uintptr_t)*ptr & 15) == 0 && *row_ld % ev == 0 && w % ev == 0) return false;
+    op[count] = {*ptr, nullptr, *row_ld, n, matrix, w, padded(w)};
     at[count] = bytes;
-    bytes += ((size_t)n * wp[count] * es + 255) & ~(size_t)255;
+    bytes += ((size_t)n * padded(w) * es + 255) & ~(size_t)255;
     p[count] = ptr;
     out_ld[count] = row_ld;
     ++count;
+    return true;
+  }
+  // the matrices: no more places than there are rows
+  void add_matrices(GroupArgs* g) {
+    const int64_t places = std::min<int64_t>(g->groups, g->n);
+    g->a_by_row = add(&g->a, &g->lda, places * g->m, g->k, g->m) && places < g->groups;
   }
   void place(char* ws) {
     for (int i = 0; i < count; ++i) {
-      dst[i] = ws + at[i];
-      *p[i] = dst[i];
-      *out_ld[i] = wp[i];
+      op[i].dst = ws + at[i];
+      *p[i] = op[i].dst;
+      *out_ld[i] = op[i].wp;
     }
   }
 };
@@ -172,12 +171,12 @@ extern "C" pbg_status pbg_group_linear(pbg_ctx* ctx, int32_t dtype, const void* 
     return set_err(ctx, PBG_ERR_INVALID_ARG, "y overlaps an input");
   st = ensure_edge_flags(ctx);
   if (st != PBG_OK) return st;
-  GroupArgs g{x, a, nullptr, y, ldx, in_dim, 0, ldy, 0, offsets, groups, n, in_dim, out_dim, in_dim, out_dim,
+  GroupArgs g{x, a, nullptr, y, ldx, in_dim, 0, ldy, 0, offsets, groups, n, in_dim, out_dim, in_dim, out_dim, false,
               ctx->edge_flag, ctx->edge_hflag};
   Operands ops(dtype);
   if (n > 0) {
     ops.add(&g.x, &g.ldx, n, in_dim);
-    ops.add(&g.a, &g.lda, (int64_t)groups * out_dim, in_dim);
+    ops.add_matrices(&g);
   }
   GroupPlan plan = plan_group(dtype, GP_FORWARD, n, groups, out_dim, in_dim, false);
   st = workspace(ctx, ops.bytes + plan.bytes());
@@ -188,7 +187,7 @@ extern "C" pbg_status pbg_group_linear(pbg_ctx* ctx, int32_t dtype, const void* 
   g.a_group = (int64_t)out_dim * g.lda;
   ctx->edge_dirty = true;
   launch_group_plan(plan, offsets, groups, n, ctx->edge_flag, ctx->cs);
-  launch_group_pack(dtype, ops.count, ops.src, ops.dst, ops.ld, ops.rows, ops.width, ops.wp, ctx->cs);
+  launch_group_pack(dtype, ops.count, ops.op, offsets, groups, ctx->cs);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) {
     launch_group_product(g, dtype, GP_FORWARD, plan, ctx->cs);
@@ -221,14 +220,14 @@ extern "C" pbg_status pbg_group_linear_backward(pbg_ctx* ctx, int32_t dtype, con
   if (!dx && !da) return PBG_OK;
   st = ensure_edge_flags(ctx);
   if (st != PBG_OK) return st;
-  GroupArgs g{x, a, dy, nullptr, ldx, in_dim, lddy, 0, 0, offsets, groups, n, in_dim, out_dim, in_dim, out_dim,
+  GroupArgs g{x, a, dy, nullptr, ldx, in_dim, lddy, 0, 0, offsets, groups, n, in_dim, out_dim, in_dim, out_dim, false,
               ctx->edge_flag, ctx->edge_hflag};
   Operands ops(dtype);
   GroupPlan plan = plan_group(dtype, dx ? GP_DX : GP_DA, n, groups, out_dim, in_dim, da != nullptr);
   if (n > 0) {
     ops.add(&g.dy, &g.lddy, n, out_dim);
     if (da) ops.add(&g.x, &g.ldx, n, in_dim);
-    if (dx) ops.add(&g.a, &g.lda, gm, in_dim);
+    if (dx) ops.add_matrices(&g);
   }
   st = workspace(ctx, ops.bytes + plan.bytes() + 16 + (size_t)plan.partial_slots * out_dim * in_dim * 4);
   if (st != PBG_OK) return st;
@@ -239,7 +238,7 @@ extern "C" pbg_status pbg_group_linear_backward(pbg_ctx* ctx, int32_t dtype, con
   g.a_group = (int64_t)out_dim * g.lda;
   ctx->edge_dirty = true;
   launch_group_plan(plan, offsets, groups, n, ctx->edge_flag, ctx->cs);
-  launch_group_pack(dtype, ops.count, ops.src, ops.dst, ops.ld, ops.rows, ops.width, ops.wp, ctx->cs);
+  launch_group_pack(dtype, ops.count, ops.op, offsets, groups, ctx->cs);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && dx) {
     g.out = dx;
