@@ -113,6 +113,14 @@ def _values(tensors, what):
     raise TypeError(f"{what} must be tensors")
 
 
+def _count(n, what):
+    """A number that the library takes as 32 bits and would see the low ones alone of.  (Widths need no such check: row
+    strides, which bound them, are 64 bits.)"""
+    if n > 0x7FFFFFFF:
+        raise ValueError(f"{what} out of range: {n}")
+    return n
+
+
 def _matrices(a, dtype, what):
     if not isinstance(a, torch.Tensor) or a.dim() != 3:
         raise ValueError(f"{what} must be [groups, out_dim, in_dim]")
@@ -127,6 +135,7 @@ def pbg_group_linear(ctx, x, a, offsets, y):
     if x.dim() != 2:
         raise ValueError("x must be [n, in_dim]")
     groups, m, k = a.shape
+    _count(groups, "groups")
     n = x.shape[0]
     xp, ldx = _rows(x, dt, (n, k), "x")
     yp, ldy = _rows(y, dt, (n, m), "y")
@@ -146,6 +155,7 @@ def pbg_group_linear_backward(ctx, x, a, offsets, dy, dx=None, da=None):
     ap = None if a is None else _matrices(a, dt, "a")
     dap = None if da is None else _matrices(da, dt, "da")
     groups, rows, k = (a if a is not None else da).shape
+    _count(groups, "groups")
     if rows != m or (a is not None and da is not None and a.shape != da.shape):
         raise ValueError(f"a and da must be [groups, {m}, in_dim]")
     xp, ldx = _rows(x, dt, (n, k), "x") if x is not None else (None, k)
@@ -166,7 +176,7 @@ def pbg_preference_loss(ctx, logits, labels, offsets, ref_logp, beta, smoothing,
     if logits.dim() != 2:
         raise ValueError("logits must be [n, candidates]")
     n, cands = logits.shape
-    pairs = (offsets.numel() - 1) // 2
+    pairs = _count((offsets.numel() - 1) // 2, "pairs")
     lp, ld = _rows(logits, dt, (n, cands), "logits")
     f = torch.float32
     args = (_vector(labels, torch.int32, n, "labels"), _vector(offsets, torch.int64, 2 * pairs + 1, "offsets"), pairs,
@@ -183,7 +193,7 @@ def pbg_preference_loss_backward(ctx, logits, labels, offsets, row_stats, dlogp,
     if logits.dim() != 2:
         raise ValueError("logits must be [n, candidates]")
     n, cands = logits.shape
-    pairs = (offsets.numel() - 1) // 2
+    pairs = _count((offsets.numel() - 1) // 2, "pairs")
     lp, ld = _rows(logits, dt, (n, cands), "logits")
     dp, lddl = _rows(dlogits, dt, (n, cands), "dlogits")
     f = torch.float32
