@@ -15,8 +15,6 @@ import torch
 from . import pbg
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-MAX_LD = 1 << 20       # PBG_OPS_MAX_LD
-MAX_DIM = 1 << 16      # PBG_OPS_MAX_DIM
 
 # every entry point the header declares
 EXPORTS = ("pbg_group_linear", "pbg_group_linear_backward", "pbg_preference_loss", "pbg_preference_loss_backward",
