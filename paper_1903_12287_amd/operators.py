@@ -119,6 +119,12 @@ def _count(n, what):
     return n
 
 
+def _pairs(offsets):
+    if not isinstance(offsets, torch.Tensor):
+        raise TypeError("offsets must be a torch.Tensor")
+    return _count((offsets.numel() - 1) // 2, "pairs")
+
+
 def _matrices(a, dtype, what):
     if not isinstance(a, torch.Tensor) or a.dim() != 3:
         raise ValueError(f"{what} must be [groups, out_dim, in_dim]")
@@ -174,7 +180,7 @@ def pbg_preference_loss(ctx, logits, labels, offsets, ref_logp, beta, smoothing,
     if logits.dim() != 2:
         raise ValueError("logits must be [n, candidates]")
     n, cands = logits.shape
-    pairs = _count((offsets.numel() - 1) // 2, "pairs")
+    pairs = _pairs(offsets)
     lp, ld = _rows(logits, dt, (n, cands), "logits")
     f = torch.float32
     args = (_vector(labels, torch.int32, n, "labels"), _vector(offsets, torch.int64, 2 * pairs + 1, "offsets"), pairs,
@@ -191,7 +197,7 @@ def pbg_preference_loss_backward(ctx, logits, labels, offsets, row_stats, dlogp,
     if logits.dim() != 2:
         raise ValueError("logits must be [n, candidates]")
     n, cands = logits.shape
-    pairs = _count((offsets.numel() - 1) // 2, "pairs")
+    pairs = _pairs(offsets)
     lp, ld = _rows(logits, dt, (n, cands), "logits")
     dp, lddl = _rows(dlogits, dt, (n, cands), "dlogits")
     f = torch.float32
