@@ -3,14 +3,19 @@
 The operators on a caller's own tensors: grouped matrix products, the preference loss and gradient clipping.  As in
 pbg.py every function has the name of its C entry point, checks dtypes, devices, shapes and layouts, passes raw
 pointers and raises pbg.PbgError when the call returns an error status.  Contexts come from pbg.pbg_bucket_init.
+
+Nothing is recorded for autograd: gradients are had by calling the _backward functions.  Written tensors count as
+modified in place, so that autograd notices where it has saved one of them for a graph of its own.
 """
 
 from __future__ import annotations
 
 import array
 import ctypes
+import math
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import pbg
 
@@ -146,6 +151,7 @@ def pbg_group_linear(ctx, x, a, offsets, y):
     op = _vector(offsets, torch.int64, groups + 1, "offsets")
     _here(x, a, offsets, y)
     _check(ctx, library().pbg_group_linear(ctx, TYPES[dt], xp, ldx, ap, op, groups, n, k, m, yp, ldy))
+    increment_version(y)   # the library writes through pointers, of which autograd sees nothing
 
 
 def pbg_group_linear_backward(ctx, x, a, offsets, dy, dx=None, da=None):
@@ -171,6 +177,7 @@ def pbg_group_linear_backward(ctx, x, a, offsets, dy, dx=None, da=None):
     _here(x, a, offsets, dy, dx, da)
     _check(ctx, library().pbg_group_linear_backward(ctx, TYPES[dt], xp, ldx, ap, dyp, lddy, op, groups, n, k, m, dxp,
                                                     lddx, dap))
+    increment_version([t for t in (dx, da) if t is not None])
 
 
 def pbg_preference_loss(ctx, logits, labels, offsets, ref_logp, beta, smoothing, loss, logp, dlogp, row_stats):
@@ -189,6 +196,7 @@ def pbg_preference_loss(ctx, logits, labels, offsets, ref_logp, beta, smoothing,
             _vector(dlogp, f, 2 * pairs, "dlogp", True), _vector(row_stats, f, 2 * n, "row_stats"))
     _here(logits, labels, offsets, ref_logp, loss, logp, dlogp, row_stats)
     _check(ctx, library().pbg_preference_loss(ctx, TYPES[dt], lp, ld, *args))
+    increment_version([t for t in (loss, logp, dlogp, row_stats) if t is not None])
 
 
 def pbg_preference_loss_backward(ctx, logits, labels, offsets, row_stats, dlogp, dlogits):
@@ -205,12 +213,13 @@ def pbg_preference_loss_backward(ctx, logits, labels, offsets, row_stats, dlogp,
             n, cands, _vector(row_stats, f, 2 * n, "row_stats"), _vector(dlogp, f, 2 * pairs, "dlogp"))
     _here(logits, labels, offsets, row_stats, dlogp, dlogits)
     _check(ctx, library().pbg_preference_loss_backward(ctx, TYPES[dt], lp, ld, *args, dp, lddl))
+    increment_version(dlogits)
 
 
 def pbg_clip_gradients(ctx, grads, max_norm, outs=None) -> float:
     """grads: tensors of any shapes (contiguous; float32, bfloat16, float16 mixed); outs: as many tensors of their types
     and sizes, or None to scale in place.  Returns the joint norm before the scaling."""
-    n = len(grads)
+    n, bound = len(grads), float(max_norm)
     if outs is not None and len(outs) != n:
         raise ValueError("one output per gradient")
     types, counts, gp = _values(grads, "grads")
@@ -221,6 +230,10 @@ def pbg_clip_gradients(ctx, grads, max_norm, outs=None) -> float:
             raise ValueError("every output must have its gradient's type and number of values")
     at = lambda v: None if v is None else v.buffer_info()[0]   # the arrays live until the call has returned
     norm = ctypes.c_double(0.0)
-    _check(ctx, library().pbg_clip_gradients(ctx, n, at(types), at(counts), at(gp), at(op), float(max_norm),
+    _check(ctx, library().pbg_clip_gradients(ctx, n, at(types), at(counts), at(gp), at(op), bound,
                                              ctypes.byref(norm)))
+    if outs is not None:
+        increment_version(outs)
+    elif norm.value > bound and math.isfinite(norm.value):
+        increment_version(grads)
     return norm.value
