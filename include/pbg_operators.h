@@ -70,10 +70,12 @@ pbg_status pbg_group_linear_backward(pbg_ctx* ctx, int32_t dtype, const void* x,
  *   row_stats[t] = (largest score m of row t, log sum_v exp(logits[t, v] - m)); (0, 0) where y_t < 0, (-inf, 0) where
  *               every score is -inf; left as it is for rows outside every sequence
  * ref_logp [2 pairs] float32 (the frozen model's logp; NULL: zeros); loss [pairs], logp, dlogp [2 pairs] and
- * row_stats [n x 2] are float32; loss and dlogp may be NULL (a frozen model's pass).  Infinities and NaN in scores that
- * count reach the results by the formulas.  offsets [2 pairs + 1] int64 as in pbg_group_linear; beta finite,
- * smoothing in [0, 1); candidates <= PBG_OPS_MAX_LD; pairs in [1, PBG_OPS_MAX_GROUPS / 2]; n < 2^24.  INVALID_ARG for
- * bad offsets and for a label of a row inside a sequence that is >= candidates. */
+ * row_stats [n x 2] are float32; loss and dlogp may be NULL (a frozen model's pass).  A score of NaN or +inf in a row
+ * that counts makes the row's log sum NaN (sums go over exp(logits[t, v] - m), and inf - inf is no number), and with it
+ * l_t, logp[q] and its pair's loss, dlogp and gradients; a label that is left out gives l_t = -inf.  offsets [2 pairs + 1]
+ * int64 as in pbg_group_linear; beta finite, smoothing in [0, 1); candidates <= PBG_OPS_MAX_LD; pairs in
+ * [1, PBG_OPS_MAX_GROUPS / 2]; n < 2^24.  INVALID_ARG for bad offsets and for a label of a row inside a sequence that is
+ * >= candidates. */
 pbg_status pbg_preference_loss(pbg_ctx* ctx, int32_t dtype, const void* logits, int64_t ld, const int32_t* labels,
                                const int64_t* offsets, int32_t pairs, int64_t n, int32_t candidates,
                                const float* ref_logp, float beta, float smoothing, float* loss, float* logp,
