@@ -284,8 +284,11 @@ __device__ __forceinline__ void row_gradient(const PrefArgs& p, int64_t t, int p
     }
     return;
   }
+  // exp(x - m) times exp(-ls), not exp((x - m) - ls): a second difference of about ten would be rounded by what is more
+  // than the whole error of the rest
+  const float inverse = (float)exp(-(double)ls);
   auto slope = [&](float x, int v) {
-    const float pr = exp_of<TYPE>((x - m) - ls);
+    const float pr = exp_of<TYPE>(x - m) * inverse;
     return (T)(g * ((v == label ? 1.0f : 0.0f) - pr));
   };
   for (int v0 = first; v0 < last; v0 += THREADS * N * U) {
