@@ -9,8 +9,8 @@
 // gradients, and a scaled value is rounded once, to its own type.
 //
 // Measured: 620 million float32 values (2.48 GB) 418 us for the squares (5.9 TB/s) and 907 for the scaling (5.5 TB/s
-// read and written; a large copy reaches 5.1); 56 tensors of 50 million values of two types 22 and 41 us, the second
-// read mostly from the cache, 5 for the factor between them.
+// read and written; a large copy reaches 5.1); 56 tensors of 50 million values of two types 21 and 41 us, the second
+// read mostly from the cache, 4 for the factor between them.
 #include "operators_device.h"
 
 namespace {

@@ -9,15 +9,17 @@
 // checks them all in one load, and small products need no kernel ahead of them.
 //
 // Measured and what bounds it (us; the product alone, without the call's 15):
-//   float32, 1,345 groups, 40,000 rows, 400 x 400, y: 261.  989 MB at 4.3 TB/s of 5.1 that a copy reaches; 52 TFLOP/s.
+//   float32, 1,345 groups of sizes as 1 / rank^1.2 (1,272 have rows), 40,000 rows, 400 x 400, y: 256.  942 MB at 3.7 TB/s
+//     of 5.1 that a copy reaches; 50 TFLOP/s.  55 % of the slots' rows are filled, and of the 40,000 rows 28,500 lie in
+//     groups of 128 and more, which read their matrix once every 32 rows.
 //   bfloat16, 32 groups, 32,768 rows, 2,048 to 4,096, y: 560, 980 TFLOP/s; one group: 500, 1,100.  A large library
 //     product reaches 1,370.  The slices' way from memory bounds it: the loads alone, nothing multiplied, take as long
 //     (585; 389 where all operands lie in the cache beside the memory), while LDS reads are hidden and products alone
 //     take 425.  Two slices of 64 KB are what the LDS holds, and a slice waits for its slowest row.  What did not help:
 //     reading ahead into the L2 (4 or 16 bytes a line, a slice or four ahead), padded rows, a persistent workgroup
 //     that fetches the next tile's slices before it stores (1 to 5 %).
-//   bfloat16, 32 groups, 16,384 rows, 2,048 x 2,048: dx 195 (705 TFLOP/s), da 245 (560; 268 MB written).
-//   float16, 24 rows in 16 groups, 2,048 x 2,048, y: 18, 134 MB of matrices read at 7.5 TB/s (partly from the cache).
+//   bfloat16, 32 groups, 16,384 rows, 2,048 x 2,048: dx 188 (730 TFLOP/s), da 230 (600; 268 MB written).
+//   float16, 24 rows in 16 groups, 2,048 x 2,048, y: 20, 134 MB of matrices read at 6.6 TB/s (partly from the cache).
 #include <algorithm>
 
 #include "operators_tile.h"
@@ -237,8 +239,9 @@ __global__ __launch_bounds__(256) void group_join_kernel(GroupArgs g, Launch L) 
 // Copies rows of `width` values into rows of `wp` >= width, a multiple of 16 bytes, with zeros behind them.  Only what
 // the products read is copied: the rows between the first and the last offset, and the matrices of groups that have
 // rows.  Where there are fewer rows than groups, a matrix's place is its group's first row, so that the copies take no
-// more than a matrix a row, however many groups there are.  Offsets that are not in order only choose which of the
-// groups' matrices are copied to which places: they have not been checked here.
+// more than a matrix a row, however many groups there are (float16, 24 rows in 400 groups, 501 x 333, y: 36 us; 76 with
+// every matrix copied).  Offsets that are not in order only choose which of the groups' matrices are copied to which
+// places: they have not been checked here.
 struct PackArgs {
   GroupPack op[3];
   uint32_t first[4];   // first workgroup of each
@@ -351,7 +354,10 @@ void launch_da(const GroupArgs& g, const GroupPlan& p, Launch L, hipStream_t s) 
 // busier (8 groups, 40,000 rows, 100 x 100: both gradients 75 us by 128 x 128, 70 by 64 x 64); in 16 bits reading the
 // operands does (128 x 128 / 256 x 256, of 2,048 x 2,048: 32 groups of 512 rows 267 / 248 us, of 2,048 rows 610 / 535,
 // uneven ones 672 / 566; where groups have to be cut to give every compute unit a tile, 4 groups of 4,096 rows:
-// 153 / 258).
+// 153 / 258).  On either side of the two lines, both gradients, us, even sizes, then sizes as 1 / rank^0.8: 32 groups of
+// 2,048 x 2,048, of 256 rows 321 / 305, 329 / 334, of 384 rows 385 / 370, 394 / 394, of 576 rows 492 / 470, 494 / 475;
+// 576 rows each, 64 groups of 512 x 512 (256 tiles) 101 / 188, 125 / 153, 8 of 2,048 x 2,048 (512 tiles) 136 / 132,
+// 142 / 141, 32 of 1,024 x 1,024 (512 tiles) 150 / 151, 155 / 180, 128 of them (2,048 tiles) 541 / 510, 560 / 572.
 int da_tile(int type, int64_t n, int64_t groups, int64_t m, int64_t k) {
   if (type == OT_F32) return 64;
   return n / groups >= 512 && groups * tiles_of(m, 256) * tiles_of(k, 256) >= 512 ? 256 : 128;
@@ -464,8 +470,11 @@ void launch_group_plan(const GroupPlan& p, const int64_t* offsets, int groups, i
 
 GroupPlan plan_group(int type, int which, int64_t n, int groups, int64_t m, int64_t k, bool want_da) {
   GroupPlan p{};
-  // Tables written ahead cost a launch (2.5 us), offsets read by every workgroup 0.5 us for each workgroup that follows
-  // another on its compute unit: 2 of 38 us saved for 24 float16 rows of 2,048, 7 of 443 lost for 16,384 bfloat16 rows.
+  // Tables written ahead cost a launch (2 us), offsets read by every workgroup 0.5 us for each workgroup that follows
+  // another on its compute unit.  Without / with tables, us: y in float32, 128 x 128, 32 groups, 8,192 rows 23 / 25,
+  // 131,072 (2^24) 72 / 74, 524,288 204 / 199, 2^20 378 / 368; float16, 2,048 x 2,048, 8 rows 38 / 40, 8,192 (2^24)
+  // 128 / 130, 32,768 327 / 322; bfloat16, 512 x 512, 2^15 rows 48 / 50, 2^18 234 / 236; both gradients in float16, 32 of
+  // 2,048 x 2,048, 2,048 rows 238 / 227 (many tiles of da for few rows), 16,384 453 / 453.
   p.tables = groups > 63 || n * std::max(m, k) > 1 << 24;
   if (which != GP_DA) {
     p.rows.shift = row_shift(type, n, groups, which == GP_FORWARD ? m : k);
