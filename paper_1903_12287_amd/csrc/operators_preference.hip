@@ -20,9 +20,8 @@
 
 namespace {
 
-// exp(d), d <= 0: base 2 through the hardware, whose argument d log2(e) is rounded.  Float32 scores get the rest back:
-// their gradient keeps more than 16 bits.  For 16-bit scores the result is off by up to |d| half steps of float32, which
-// a 16-bit gradient does not hold, and which in a sum that is one or more counts |d| e^-|d|, at most 0.37 of a half step.
+// exp(d), d <= 0: base 2 through the hardware, whose argument d log2(e) is rounded.  Float32 results get the rest back;
+// gradients of 16 bits do not hold it (|d| half steps of float32).
 template <int TYPE>
 __device__ __forceinline__ float exp_of(float d) {
   constexpr float L = 1.44269502f, LL = 1.92596299e-8f;   // log2(e) in two parts
@@ -40,33 +39,29 @@ struct Stats {
 };
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
 
-template <int TYPE>
-__device__ __forceinline__ void join(Stats& a, const Stats& b) {
-  const float m = fmaxf(a.m, b.m), base = base_of(m);
-  a.s = a.s * exp_of<TYPE>(a.m - base) + b.s * exp_of<TYPE>(b.m - base);
-  a.m = m;
-}
+// a set's sum relative to `base`, its largest score or above: all of the sum is off by what this exp is, so it keeps
+// float32 whatever the scores' type.  (Without: 2e-8 to 7e-8 of the sums to one side, growing with the row.)
+__device__ __forceinline__ float sum_at(const Stats& a, float base) { return a.s * exp_of<OT_F32>(a.m - base); }
 
 // Scores of 16 bits take exp(x - m) as 2^(x log2(e) - M), M = m log2(e) rounded: one multiply-add and its rounding.  What
 // M's rounding left out is the same for every term and comes off the sum; what float32 leaves out of log2(e) stays and
 // makes a term too large by 1.3e-8 |x - m| of itself.  (Log sums of 300 to 131,001 normal scores are off by 7e-8 to
-// 1.2e-7, root mean square, their own rounding to float32 included, 2e-8 to 7e-8 of it to one side; with log2(e) in two
-// parts and exp_of's rest in the joins 7e-8 to 1.0e-7, but 96 rows of 131,001 took 36 us for 33.)  Far from zero (where M's
-// rounding would no longer be small) and in float32 the difference is formed first.
+// 1.0e-7, root mean square, their own rounding to float32 included, as with log2(e) in two parts.)  Far from zero (where
+// M's rounding would no longer be small) and in float32 the difference is formed first.
 template <int TYPE, int COUNT>
 __device__ __forceinline__ void add_scores(Stats& a, const float (&x)[COUNT]) {
   float m = a.m;
 #pragma unroll
   for (int i = 0; i < COUNT; ++i) m = fmaxf(m, x[i]);
   const float base = base_of(m);
-  const float old = a.s * exp_of<TYPE>(a.m - base);
+  const float old = sum_at(a, base);
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   if (TYPE != OT_F32 && fabsf(base) < 65536.0f * 16.0f) {
     constexpr float L = 1.44269502f;
     const float M = base * L;
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) s[i & 3] += __builtin_amdgcn_exp2f(fmaf(x[i], L, -M));
-    const float left = fmaf(base, L, -M);   // exact
+    const float left = fmaf(base, L, -M);
     a.s = fmaf((s[0] + s[1]) + (s[2] + s[3]), __builtin_amdgcn_exp2f(-left), old);
   } else {
 #pragma unroll
@@ -112,24 +107,22 @@ __device__ __forceinline__ Stats scan(const typename Elem<TYPE>::T* z, int first
     }
     add_scores<TYPE>(a, x);
   }
+  float m = a.m;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const Stats b = {__shfl_xor(a.m, o, 64), __shfl_xor(a.s, o, 64)};
-    join<TYPE>(a, b);
-  }
-  return a;
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  float s = sum_at(a, base_of(m));
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  return {m, s};
 }
 
-// a workgroup's stats from its waves', in thread 0
-template <int TYPE>
-__device__ __forceinline__ Stats join_waves(Stats a) {
+// a workgroup's stats from its waves'
+__device__ __forceinline__ Stats join_waves(const Stats& a) {
   __shared__ Stats part[4];
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = a;
   __syncthreads();
-  a = part[0];
-#pragma unroll
-  for (int w = 1; w < 4; ++w) join<TYPE>(a, part[w]);
-  return a;
+  const float m = fmaxf(fmaxf(part[0].m, part[1].m), fmaxf(part[2].m, part[3].m)), base = base_of(m);
+  return {m, (sum_at(part[0], base) + sum_at(part[1], base)) + (sum_at(part[2], base) + sum_at(part[3], base))};
 }
 
 // a counted row's stats and log probability; a row without a distribution does not count.  The logarithm is taken in
@@ -164,7 +157,7 @@ __global__ __launch_bounds__(256) void row_stats_kernel(PrefArgs p) {
   const float z_label = (float)z[label];
   Stats a;
   if (WAVE) a = scan<TYPE, 64>(z, 0, p.V, tid);
-  else a = join_waves<TYPE>(scan<TYPE, 256>(z, 0, p.V, tid));
+  else a = join_waves(scan<TYPE, 256>(z, 0, p.V, tid));
   if (tid) return;
   float2 st;
   finish_row(a, z_label, st, p.picked[t]);
@@ -195,7 +188,7 @@ __global__ __launch_bounds__(256) void row_parts_kernel(PrefArgs p) {
   if (label < 0 || label >= p.V) return;
   const int per = ((p.V + p.splits - 1) / p.splits + 255) & ~255;
   const int first = min(p.V, part * per), last = min(p.V, first + per);
-  const Stats a = join_waves<TYPE>(scan<TYPE, 256>((const T*)p.logits + t * p.ld, first, last, tid));
+  const Stats a = join_waves(scan<TYPE, 256>((const T*)p.logits + t * p.ld, first, last, tid));
   if (tid == 0) ((Stats*)p.parts)[blockIdx.x] = a;
 }
 
@@ -223,9 +216,13 @@ __global__ __launch_bounds__(1024) void pair_loss_kernel(PrefArgs p) {
             Stats b[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) b[i] = q[min(i0 + i, p.splits - 1)];
+            float m = a.m;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (i0 + i < p.splits) join<TYPE>(a, b[i]);
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, b[i].m);
+            const float base = base_of(m);
+            a = {m, sum_at(a, base)};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a.s += i0 + i < p.splits ? sum_at(b[i], base) : 0.0f;
           }
           finish_row(a, z_label, st, l);
         }
