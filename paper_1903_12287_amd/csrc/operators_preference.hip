@@ -13,7 +13,7 @@
 // Measured, bfloat16, 16,384 rows of 15,000 candidates, a fifth of them without a label: 69 us for the sums by
 // themselves (393 MB, 5.7 TB/s; an exponential a score), 108 right behind a gradient whose writes are still on their way
 // to memory, as in a loop of both; 154 for the gradient (393 MB read, 492 written, 5.7 TB/s; a large copy reaches 5.1).
-// float16, 96 rows of 131,001: 9 us for the parts, 9 to join them.
+// float16, 96 rows of 131,001: 9 us for the parts, 8 to join them.
 #include <algorithm>
 
 #include "operators_device.h"
